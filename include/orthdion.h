@@ -286,6 +286,116 @@ size_t orthdion_static_scratch_bytes(void);
 int orthdion_step_static(orthdion_handle h, void* const* X, const void* const* G, float* const* M,
                          float* const* Q, void* stream);
 
+/* ==== Muon: the full-rank counterpart of the step above, for matrices whose whole momentum is
+ * orthogonalised.  For every matrix of the set (paper letters do not apply; the method is the
+ * published Muon optimizer, the paper's comparison system of Sec. 6):
+ *
+ *   M    = mu M + G                    momentum
+ *   B    = G + mu M | M                Nesterov | heavy ball
+ *   X_0  = B / (||B||_F + eps)
+ *   X_k+1 = a X_k + (b S + c S S) X_k,  S = X_k X_k^T,     k = 0 .. steps - 1 (Newton-Schulz)
+ *   X    = (1 - lr weight_decay) X - lr scale X_steps
+ *
+ * With the published coefficients (3.4445, -4.7750, 2.0315) and 5 steps the singular values of
+ * X_steps lie around 1; with (1.875, -1.25, 0.375) or a schedule ending in it they converge to 1,
+ * i.e. X_steps to the polar factor.  Coefficients are the caller's, one triple per step.
+ *
+ * Matrices have any m, n >= 1 below 2^22 and any row strides (ldx, ldg, ldm >= n, in elements);
+ * pointers need the alignment of their type only.  Rows whose pointers and strides are multiples
+ * of 16 bytes and 8 elements are moved faster.  A matrix is transposed on the way in where m > n.
+ *
+ * Arithmetic: accumulation is fp32, the norm fp64.  FAST: operands in fp16 under powers of two
+ * (11 bits).  EXACT: two fp16 words per value, three products (22 bits).  AUTO as for orthdion_step.
+ * A zero matrix gives X_steps = 0.  A matrix with a NaN or an infinity in B gives NaN everywhere in
+ * X (or O) and 1 in orthdion_muon_get_info; other matrices of the set are not affected.
+ *
+ * Memory, errors and streams as for orthdion_step: nothing is allocated and nothing waited for;
+ * calls of one handle on one workspace are enqueued on one stream at a time, and a call under
+ * capture is replayed with the lr, mu and weight_decay of its capture.  Every call writes all of
+ * the workspace that it reads, so several handles and captured graphs may share one in turn.
+ * Buffers of a call must not overlap each other or the workspace.  The current device is the one
+ * that the buffers and the stream belong to. */
+typedef struct orthdion_muon_ctx* orthdion_muon_handle;   /* opaque; host memory only */
+#define ORTHDION_MUON_MAX_STEPS 32
+
+typedef struct {
+  int64_t m, n;
+  int64_t ldx, ldg, ldm;
+  float scale;            /* of this matrix's update, e.g. sqrt(max(1, m / n)) */
+} orthdion_muon_matdesc;
+
+typedef struct {
+  orthdion_dtype x_dtype, g_dtype;
+  orthdion_precision precision;
+  int32_t nesterov;       /* 0 or 1 */
+  int32_t steps;          /* 1 .. ORTHDION_MUON_MAX_STEPS */
+  float coeffs[3 * ORTHDION_MUON_MAX_STEPS];   /* a, b, c of every step.  Refused (ORTHDION_E_INVALID_ARG)
+                           * where singular values in [0, 1] could grow beyond 32, or |a + b s^2 + c s^4|
+                           * beyond 256 over the range that a step may meet */
+  float mu;               /* 0 <= mu <= 1 */
+  float lr, weight_decay;
+  float eps;              /* >= 0 */
+} orthdion_muon_config;
+
+int orthdion_muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* mats, int32_t nmat,
+                         const orthdion_muon_config* cfg);
+/* Bytes of device scratch of a call, 256-byte aligned; 0 for a NULL handle. */
+size_t orthdion_muon_workspace_bytes(orthdion_muon_handle h);
+int orthdion_muon_set_lr(orthdion_muon_handle h, float lr);
+int orthdion_muon_set_mu(orthdion_muon_handle h, float mu);
+int orthdion_muon_set_weight_decay(orthdion_muon_handle h, float weight_decay);
+
+/* One step over the set: X (x_dtype, ldx) and M (fp32, ldm) are updated in place, G (g_dtype, ldg) is
+ * read.  Host arrays of nmat device pointers. */
+int orthdion_muon_step(orthdion_muon_handle h, void* const* X, const void* const* G, float* const* M,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* The orthogonalisation alone: O = X_steps of X_0 = A / (||A||_F + eps).  A is laid out as G (g_dtype,
+ * ldg), O as X (x_dtype, ldx); mu, lr, weight_decay and scale have no part in it. */
+int orthdion_muon_orthogonalise(orthdion_muon_handle h, const void* const* A, void* const* O, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/* Waits for `stream`, then writes for every matrix of the last call 0, or 1 where B (A) held a NaN or
+ * an infinity. */
+int orthdion_muon_get_info(orthdion_muon_handle h, int32_t* info_host, void* stream);
+int orthdion_muon_destroy(orthdion_muon_handle h);
+
+/* ==== AdamW with decoupled weight decay, for the tensors of a model that are no matrices of a
+ * spectral update (embeddings, output head, norm gains, biases):
+ *
+ *   t = t + 1,   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   x = (1 - lr_i wd_i) x - lr_i (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),   lr_i = lr lr_scale
+ *
+ * A tensor is a run of `length` >= 0 elements; pointers need the alignment of their type only (a
+ * tensor whose four pointers are multiples of 16 bytes is moved faster).  x is rounded to its type
+ * once, to nearest even.  No workspace. */
+typedef struct orthdion_adamw_ctx* orthdion_adamw_handle;
+
+typedef struct {
+  int64_t length;         /* below 2^42 */
+  float lr_scale, weight_decay;
+} orthdion_adamw_desc;
+
+typedef struct {
+  orthdion_dtype x_dtype, g_dtype;
+  double beta1, beta2;    /* in [0, 1); doubles, because 1 - beta and 1 - beta^t are differences of them */
+  float lr, eps;
+} orthdion_adamw_config;
+
+int orthdion_adamw_create(orthdion_adamw_handle* out, const orthdion_adamw_desc* tensors, int32_t count,
+                          const orthdion_adamw_config* cfg);
+int orthdion_adamw_set_lr(orthdion_adamw_handle h, float lr);
+
+/* One step over the list.  X (x_dtype), M and V (fp32) are updated in place, G (g_dtype) is read; host
+ * arrays of device pointers (NULL allowed where length is 0).  `counter` points to two int32 in
+ * device memory: [0] the steps taken so far (t before the call; 0 at first), advanced by the call on
+ * the device, so that a captured call counts its replays; [1] is the library's and 0 between
+ * calls.  Calls on one counter are enqueued on one stream at a time.  Only enqueues work; buffers
+ * must not overlap. */
+int orthdion_adamw_step(orthdion_adamw_handle h, void* const* X, const void* const* G, float* const* M,
+                        float* const* V, int32_t* counter, void* stream);
+int orthdion_adamw_destroy(orthdion_adamw_handle h);
+
 const char* orthdion_strerror(int status);
 
 int orthdion_destroy(orthdion_handle h);

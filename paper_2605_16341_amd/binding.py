@@ -30,7 +30,10 @@ EXPORTS = ["orthdion_create", "orthdion_workspace_bytes", "orthdion_set_lr", "or
            "orthdion_profile_begin", "orthdion_profile_end", "orthdion_set_diagnostics",
            "orthdion_get_diagnostics", "orthdion_rank_policy", "orthdion_resize_q", "orthdion_strerror",
            "orthdion_destroy", "orthdion_step_static", "orthdion_static_scratch_bytes", "orthdion_get_warnings",
-           "orthdion_get_groups"]
+           "orthdion_get_groups", "orthdion_muon_create", "orthdion_muon_workspace_bytes", "orthdion_muon_set_lr",
+           "orthdion_muon_set_mu", "orthdion_muon_set_weight_decay", "orthdion_muon_step", "orthdion_muon_orthogonalise",
+           "orthdion_muon_get_info", "orthdion_muon_destroy", "orthdion_adamw_create", "orthdion_adamw_set_lr",
+           "orthdion_adamw_step", "orthdion_adamw_destroy"]
 
 DIAG = ["b_norm", "r_norm", "tracking_error", "residual_ratio", "inner", "nu", "erank", "g_norm"]
 ORTHDION_NDIAG = len(DIAG)
@@ -49,6 +52,32 @@ class orthdion_config(ctypes.Structure):
     _fields_ = [("x_dtype", ctypes.c_int), ("g_dtype", ctypes.c_int), ("variant", ctypes.c_int),
                 ("ef", ctypes.c_int), ("precision", ctypes.c_int), ("mu", ctypes.c_float),
                 ("lr", ctypes.c_float), ("groups", ctypes.c_int32)]
+
+
+ORTHDION_MUON_MAX_STEPS = 32
+# the published quintic of the Muon optimizer, five steps
+MUON_COEFFS = ((3.4445, -4.7750, 2.0315),) * 5
+
+
+class orthdion_muon_matdesc(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_int64), ("n", ctypes.c_int64), ("ldx", ctypes.c_int64), ("ldg", ctypes.c_int64),
+                ("ldm", ctypes.c_int64), ("scale", ctypes.c_float)]
+
+
+class orthdion_muon_config(ctypes.Structure):
+    _fields_ = [("x_dtype", ctypes.c_int), ("g_dtype", ctypes.c_int), ("precision", ctypes.c_int),
+                ("nesterov", ctypes.c_int32), ("steps", ctypes.c_int32),
+                ("coeffs", ctypes.c_float * (3 * ORTHDION_MUON_MAX_STEPS)), ("mu", ctypes.c_float), ("lr", ctypes.c_float),
+                ("weight_decay", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class orthdion_adamw_desc(ctypes.Structure):
+    _fields_ = [("length", ctypes.c_int64), ("lr_scale", ctypes.c_float), ("weight_decay", ctypes.c_float)]
+
+
+class orthdion_adamw_config(ctypes.Structure):
+    _fields_ = [("x_dtype", ctypes.c_int), ("g_dtype", ctypes.c_int), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("lr", ctypes.c_float), ("eps", ctypes.c_float)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -127,6 +156,20 @@ def load() -> ctypes.CDLL:
     lib.orthdion_strerror.restype = ctypes.c_char_p
     lib.orthdion_destroy.argtypes = [vp]
     lib.orthdion_destroy.restype = ctypes.c_int
+    pp, f32 = ctypes.POINTER(vp), ctypes.c_float
+    for name, args, res in (
+            ("orthdion_muon_create", [pp, ctypes.POINTER(orthdion_muon_matdesc), ctypes.c_int32, ctypes.POINTER(orthdion_muon_config)], ctypes.c_int),
+            ("orthdion_muon_workspace_bytes", [vp], sz), ("orthdion_muon_set_lr", [vp, f32], ctypes.c_int),
+            ("orthdion_muon_set_mu", [vp, f32], ctypes.c_int), ("orthdion_muon_set_weight_decay", [vp, f32], ctypes.c_int),
+            ("orthdion_muon_step", [vp, pp, pp, pp, vp, sz, vp], ctypes.c_int),
+            ("orthdion_muon_orthogonalise", [vp, pp, pp, vp, sz, vp], ctypes.c_int),
+            ("orthdion_muon_get_info", [vp, ctypes.POINTER(ctypes.c_int32), vp], ctypes.c_int),
+            ("orthdion_muon_destroy", [vp], ctypes.c_int),
+            ("orthdion_adamw_create", [pp, ctypes.POINTER(orthdion_adamw_desc), ctypes.c_int32, ctypes.POINTER(orthdion_adamw_config)], ctypes.c_int),
+            ("orthdion_adamw_set_lr", [vp, f32], ctypes.c_int),
+            ("orthdion_adamw_step", [vp, pp, pp, pp, pp, vp, vp], ctypes.c_int), ("orthdion_adamw_destroy", [vp], ctypes.c_int)):
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = res
     _lib = lib
     return lib
 
@@ -273,6 +316,96 @@ def orthdion_destroy(handle: int) -> None:
     _check(load().orthdion_destroy(handle))
 
 
+def orthdion_muon_create(shapes: Sequence[Sequence[int]], x_dtype: int, g_dtype: int, precision: int = ORTHDION_PREC_AUTO,
+                         nesterov: bool = True, coeffs: Sequence[Sequence[float]] = MUON_COEFFS, mu: float = 0.95, lr: float = 0.02,
+                         weight_decay: float = 0.0, eps: float = 1e-7, scales: Optional[Sequence[float]] = None,
+                         lds: Optional[Sequence[Sequence[int]]] = None) -> int:
+    """`shapes` is a list of (m, n); `coeffs` one (a, b, c) per Newton-Schulz step; `scales` one factor of the update per
+    matrix (default 1); `lds` optional (ldx, ldg, ldm) per matrix (default n).  Returns the opaque handle as an int."""
+    nmat = len(shapes)
+    descs = (orthdion_muon_matdesc * max(nmat, 1))()
+    for i, (m, n) in enumerate(shapes):
+        ld = lds[i] if lds is not None else (n, n, n)
+        descs[i] = orthdion_muon_matdesc(int(m), int(n), int(ld[0]), int(ld[1]), int(ld[2]), 1.0 if scales is None else float(scales[i]))
+    flat = [float(v) for step in coeffs for v in step]
+    if len(flat) != 3 * len(coeffs) or len(coeffs) > ORTHDION_MUON_MAX_STEPS:
+        raise ValueError(f"coeffs: at most {ORTHDION_MUON_MAX_STEPS} triples (a, b, c)")
+    cfg = orthdion_muon_config(int(x_dtype), int(g_dtype), int(precision), int(nesterov), len(coeffs),
+                               (ctypes.c_float * (3 * ORTHDION_MUON_MAX_STEPS))(*flat), float(mu), float(lr), float(weight_decay), float(eps))
+    handle = ctypes.c_void_p()
+    _check(load().orthdion_muon_create(ctypes.byref(handle), descs, nmat, ctypes.byref(cfg)))
+    return handle.value
+
+
+def orthdion_muon_workspace_bytes(handle: int) -> int:
+    return int(load().orthdion_muon_workspace_bytes(handle))
+
+
+def orthdion_muon_set_lr(handle: int, lr: float) -> None:
+    _check(load().orthdion_muon_set_lr(handle, float(lr)))
+
+
+def orthdion_muon_set_mu(handle: int, mu: float) -> None:
+    _check(load().orthdion_muon_set_mu(handle, float(mu)))
+
+
+def orthdion_muon_set_weight_decay(handle: int, weight_decay: float) -> None:
+    _check(load().orthdion_muon_set_weight_decay(handle, float(weight_decay)))
+
+
+def orthdion_muon_step(handle: int, X: Sequence[int], G: Sequence[int], M: Sequence[int], workspace: int, workspace_bytes: int,
+                       stream: int = 0) -> None:
+    """X, G, M: device addresses (ints), one per matrix."""
+    _check(load().orthdion_muon_step(handle, _ptr_array(X), _ptr_array(G), _ptr_array(M), ctypes.c_void_p(workspace),
+                                     workspace_bytes, ctypes.c_void_p(stream)))
+
+
+def orthdion_muon_orthogonalise(handle: int, A: Sequence[int], O: Sequence[int], workspace: int, workspace_bytes: int,
+                                stream: int = 0) -> None:
+    _check(load().orthdion_muon_orthogonalise(handle, _ptr_array(A), _ptr_array(O), ctypes.c_void_p(workspace), workspace_bytes,
+                                              ctypes.c_void_p(stream)))
+
+
+def orthdion_muon_get_info(handle: int, nmat: int, stream: int = 0) -> List[int]:
+    out = (ctypes.c_int32 * nmat)()
+    _check(load().orthdion_muon_get_info(handle, out, ctypes.c_void_p(stream)))
+    return list(out)
+
+
+def orthdion_muon_destroy(handle: int) -> None:
+    _check(load().orthdion_muon_destroy(handle))
+
+
+def orthdion_adamw_create(lengths: Sequence[int], x_dtype: int, g_dtype: int, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999,
+                          eps: float = 1e-8, weight_decays: Optional[Sequence[float]] = None,
+                          lr_scales: Optional[Sequence[float]] = None) -> int:
+    """`lengths`: elements of every tensor; one weight decay (default 0) and factor of lr (default 1) each."""
+    count = len(lengths)
+    descs = (orthdion_adamw_desc * max(count, 1))()
+    for i, n in enumerate(lengths):
+        descs[i] = orthdion_adamw_desc(int(n), 1.0 if lr_scales is None else float(lr_scales[i]),
+                                       0.0 if weight_decays is None else float(weight_decays[i]))
+    cfg = orthdion_adamw_config(int(x_dtype), int(g_dtype), float(beta1), float(beta2), float(lr), float(eps))
+    handle = ctypes.c_void_p()
+    _check(load().orthdion_adamw_create(ctypes.byref(handle), descs, count, ctypes.byref(cfg)))
+    return handle.value
+
+
+def orthdion_adamw_set_lr(handle: int, lr: float) -> None:
+    _check(load().orthdion_adamw_set_lr(handle, float(lr)))
+
+
+def orthdion_adamw_step(handle: int, X: Sequence[int], G: Sequence[int], M: Sequence[int], V: Sequence[int], counter: int,
+                        stream: int = 0) -> None:
+    """Device addresses as ints; `counter` that of two int32, [steps taken, 0]."""
+    _check(load().orthdion_adamw_step(handle, _ptr_array(X), _ptr_array(G), _ptr_array(M), _ptr_array(V), ctypes.c_void_p(counter),
+                                      ctypes.c_void_p(stream)))
+
+
+def orthdion_adamw_destroy(handle: int) -> None:
+    _check(load().orthdion_adamw_destroy(handle))
+
+
 class OrthDion:
     """Owns a handle and a torch-allocated workspace; `step` takes lists of torch tensors
     (device memory and the current stream come from torch; nothing else does)."""
@@ -362,6 +495,160 @@ class OrthDion:
     def close(self) -> None:
         if self.handle:
             orthdion_destroy(self.handle)
+            self.handle = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _dtypes(torch, x_dtype: str, g_dtype: Optional[str]):
+    """(code, torch type) of x and g; g has x's type unless given."""
+    known = {"f32": (ORTHDION_F32, torch.float32), "bf16": (ORTHDION_BF16, torch.bfloat16)}
+    for t in (x_dtype, g_dtype or x_dtype):
+        if t not in known:
+            raise ValueError(f"dtype {t!r}: need one of {sorted(known)}")
+    return known[x_dtype], known[g_dtype or x_dtype]
+
+
+def _per_item(name: str, value, count: int) -> List[float]:
+    """One float per item from one for all or a sequence."""
+    got = [float(value)] * count if isinstance(value, (int, float)) else [float(v) for v in value]
+    if len(got) != count:
+        raise ValueError(f"{name}: expected one value or {count}, got {len(got)}")
+    return got
+
+
+class Muon:
+    """Owns a handle and a torch-allocated workspace of the Muon step; tensors are the caller's.
+
+    shapes   list of (m, n)
+    coeffs   one (a, b, c) per Newton-Schulz step
+    scale    factor of every matrix's update: "none" (1), "spectral" (sqrt(max(1, m / n))), "rms" (0.2 sqrt(max(m, n)), the
+             root mean square of an AdamW update), or a list of numbers
+    lds      (ldx, ldg, ldm) per matrix where rows are further apart than n elements, e.g. parts of a fused projection
+    """
+
+    def __init__(self, shapes, x_dtype="bf16", g_dtype=None, precision="auto", mu=0.95, lr=0.02, weight_decay=0.0, nesterov=True,
+                 coeffs=MUON_COEFFS, eps=1e-7, scale="spectral", lds=None, device="cuda:0"):
+        import torch
+        self.handle = 0
+        self._torch = torch
+        self.device = torch.device(device)
+        self.shapes = [(int(m), int(n)) for m, n in shapes]
+        self.nmat = len(self.shapes)
+        self.lds = [tuple(int(v) for v in ld) for ld in lds] if lds is not None else [(n, n, n) for _, n in self.shapes]
+        if len(self.lds) != self.nmat:
+            raise ValueError(f"lds: expected {self.nmat} triples, got {len(self.lds)}")
+        (xc, self._x_dtype), (gc, self._g_dtype) = _dtypes(torch, x_dtype, g_dtype)
+        rules = {"none": lambda m, n: 1.0, "spectral": lambda m, n: max(1.0, m / n) ** 0.5, "rms": lambda m, n: 0.2 * max(m, n) ** 0.5}
+        if isinstance(scale, str):
+            if scale not in rules:
+                raise ValueError(f"scale {scale!r}: need one of {sorted(rules)} or a list of numbers")
+            scale = [rules[scale](m, n) if m > 0 and n > 0 else 1.0 for m, n in self.shapes]
+        self.handle = orthdion_muon_create(
+            self.shapes, xc, gc, {"auto": ORTHDION_PREC_AUTO, "fast": ORTHDION_PREC_FAST, "exact": ORTHDION_PREC_EXACT}[precision],
+            nesterov, coeffs, mu, lr, weight_decay, eps, _per_item("scale", scale, self.nmat), self.lds)
+        self.workspace_bytes = orthdion_muon_workspace_bytes(self.handle)
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
+
+    def _pointers(self, **named) -> List[List[int]]:
+        """Addresses of lists of tensors, after the checks that raw addresses cannot have: one wrong type, shape, stride or
+        device would be an access out of bounds."""
+        out = []
+        for name, (seq, dtype, which) in named.items():
+            if len(seq) != self.nmat:
+                raise ValueError(f"{name}: expected {self.nmat} tensors, got {len(seq)}")
+            for i, t in enumerate(seq):
+                m, n = self.shapes[i]
+                ld = self.lds[i][which]
+                rows = t.dim() == 2 and (n == 1 or t.stride(1) == 1) and (m == 1 or t.stride(0) == ld)
+                if t.device.type != "cuda" or tuple(t.shape) != (m, n) or t.dtype != dtype or not rows:
+                    raise ValueError(f"{name}[{i}]: need a {dtype} device tensor of shape {(m, n)} with rows {ld} elements apart, got "
+                                     f"{t.dtype} {tuple(t.shape)} with strides {tuple(t.stride())} on {t.device}")
+                if t.device != self.workspace.device:
+                    raise ValueError(f"{name}[{i}]: on {t.device}, the workspace on {self.workspace.device}")
+            out.append([t.data_ptr() for t in seq])
+        return out
+
+    def _stream(self, stream) -> int:
+        return stream if stream is not None else self._torch.cuda.current_stream(self.workspace.device).cuda_stream
+
+    def step(self, X, G, M, stream=None) -> None:
+        """One optimizer step: X and M are updated in place."""
+        x, g, m = self._pointers(X=(X, self._x_dtype, 0), G=(G, self._g_dtype, 1), M=(M, self._torch.float32, 2))
+        with self._torch.cuda.device(self.workspace.device):
+            orthdion_muon_step(self.handle, x, g, m, self.workspace.data_ptr(), self.workspace_bytes, self._stream(stream))
+
+    def orthogonalise(self, A, out, stream=None) -> None:
+        """The orthogonalised A (laid out as G) into `out` (laid out as X)."""
+        a, o = self._pointers(A=(A, self._g_dtype, 1), out=(out, self._x_dtype, 0))
+        with self._torch.cuda.device(self.workspace.device):
+            orthdion_muon_orthogonalise(self.handle, a, o, self.workspace.data_ptr(), self.workspace_bytes, self._stream(stream))
+
+    def info(self, stream=None) -> List[int]:
+        return orthdion_muon_get_info(self.handle, self.nmat, self._stream(stream))
+
+    def set_lr(self, lr: float) -> None:
+        orthdion_muon_set_lr(self.handle, lr)
+
+    def set_mu(self, mu: float) -> None:
+        orthdion_muon_set_mu(self.handle, mu)
+
+    def set_weight_decay(self, weight_decay: float) -> None:
+        orthdion_muon_set_weight_decay(self.handle, weight_decay)
+
+    def close(self) -> None:
+        if self.handle:
+            orthdion_muon_destroy(self.handle)
+            self.handle = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class AdamW:
+    """Owns a handle of the AdamW step over a list of tensors; `lengths` are their numbers of elements.  `weight_decay` and
+    `lr_scale` are one number or one per tensor."""
+
+    def __init__(self, lengths, x_dtype="bf16", g_dtype=None, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, lr_scale=1.0):
+        import torch
+        self.handle = 0
+        self._torch = torch
+        self.lengths = [int(n) for n in lengths]
+        count = len(self.lengths)
+        (xc, self._x_dtype), (gc, self._g_dtype) = _dtypes(torch, x_dtype, g_dtype)
+        self.handle = orthdion_adamw_create(self.lengths, xc, gc, lr, betas[0], betas[1], eps,
+                                            _per_item("weight_decay", weight_decay, count), _per_item("lr_scale", lr_scale, count))
+
+    def step(self, X, G, M, V, counter, stream=None) -> None:
+        """One step: X, M and V are updated in place.  `counter` is an int32 tensor of two on the tensors' device, [steps taken
+        so far, 0]; the step advances it there."""
+        torch = self._torch
+        if counter.device.type != "cuda" or counter.dtype != torch.int32 or tuple(counter.shape) != (2,) or not counter.is_contiguous():
+            raise ValueError(f"counter: need an int32 device tensor of two, got {counter.dtype} {tuple(counter.shape)} on {counter.device}")
+        for name, seq, dtype in (("X", X, self._x_dtype), ("G", G, self._g_dtype), ("M", M, torch.float32), ("V", V, torch.float32)):
+            if len(seq) != len(self.lengths):
+                raise ValueError(f"{name}: expected {len(self.lengths)} tensors, got {len(seq)}")
+            for i, t in enumerate(seq):
+                if t.device != counter.device or t.dtype != dtype or t.numel() != self.lengths[i] or not t.is_contiguous():
+                    raise ValueError(f"{name}[{i}]: need a contiguous {dtype} tensor of {self.lengths[i]} elements on {counter.device}, got "
+                                     f"{t.dtype} {tuple(t.shape)} on {t.device}, contiguous={t.is_contiguous()}")
+        with torch.cuda.device(counter.device):
+            orthdion_adamw_step(self.handle, *([t.data_ptr() for t in seq] for seq in (X, G, M, V)), counter.data_ptr(),
+                                stream if stream is not None else torch.cuda.current_stream(counter.device).cuda_stream)
+
+    def set_lr(self, lr: float) -> None:
+        orthdion_adamw_set_lr(self.handle, lr)
+
+    def close(self) -> None:
+        if self.handle:
+            orthdion_adamw_destroy(self.handle)
             self.handle = 0
 
     def __del__(self):

@@ -9,7 +9,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liborthdion.so")
-SOURCES = ["od_kernels.hip", "od_diag.hip", "od_static.hip", "od_api.cpp"]
+SOURCES = ["od_kernels.hip", "od_diag.hip", "od_static.hip", "od_muon.hip", "od_adamw.hip", "od_api.cpp", "od_muon_api.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function"]

@@ -1087,7 +1087,7 @@ extern "C" const char* orthdion_strerror(int status) {
     case ORTHDION_OK: return "ok";
     case ORTHDION_E_INVALID_ARG: return "invalid argument";
     case ORTHDION_E_NULL_PTR: return "null pointer";
-    case ORTHDION_E_BAD_SHAPE: return "unsupported shape: m, n, r, ld must be multiples of 8 with 8 <= r <= min(m, n) and ld >= n";
+    case ORTHDION_E_BAD_SHAPE: return "unsupported shape: m, n, r, ld must be multiples of 8 with 8 <= r <= min(m, n) and ld >= n (Muon: m, n >= 1 and ld >= n; AdamW: length >= 0)";
     case ORTHDION_E_WORKSPACE_TOO_SMALL: return "workspace too small";
     case ORTHDION_E_MISALIGNED: return "device pointer not sufficiently aligned";
     case ORTHDION_E_HIP: return "HIP call failed";

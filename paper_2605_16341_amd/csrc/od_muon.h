@@ -1,0 +1,79 @@
+// Launchers of the Muon kernels (od_muon.hip): momentum and scaling of the input, the products of the
+// Newton-Schulz iteration, the parameter update.  Every launcher only enqueues work on `stream`.
+//
+// A matrix A (m x n) is worked on as Y (p x q) with p = min(m, n), q = max(m, n): A itself or its transpose.
+// Its slice of the workspace holds fp16 operand words only, `parts` planes (1: the value under a power-of-two
+// scale, 2: hi + lo of it) of
+//   Y twice (read by one iteration, written for the next)   pp rows of lq, rows p .. pp and columns q .. qq zero
+//   S = Y Y^T and P = a I + b S + c S S                     p rows of lp, columns p .. pp zero
+// with pp and qq the multiples of 64 above p and q: the K loops run over whole 64-deep steps unchecked.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace od {
+
+constexpr int kNsStep = 64;                // k of one step of the K loops
+constexpr int kNsClasses = 16;             // classes (matrices of one shape) that share a launch
+constexpr int kMuonChunk = 48;             // matrices whose pointers travel in one launch's arguments
+constexpr int kMuonParts = 256;            // most partial sums of squares of one matrix
+
+// caller's buffers of one matrix; O and A of orthdion_muon_orthogonalise stand at X and G, M is null
+struct MuonEntry {
+  void* X;
+  const void* G;
+  float* M;
+};
+
+struct MuonMat {                           // one matrix, as the elementwise kernels see it
+  int m, n;
+  int64_t ldx, ldg, ldm;
+  float scale;                             // of its update
+  int blocks;                              // partial sums
+};
+
+// One class in a launch over several: nb matrices of p x q (or q x p where tall).
+struct NsClass {
+  int first;                               // first workgroup of the class
+  int p, q, lp, lq, nb;
+  int mat0;                                // first row of the class in the matrix tables
+  int tall;
+  uint16_t* base;                          // slice of its first matrix
+  int64_t stride;                          // elements between slices
+};
+
+struct NsArgs {
+  int nclass, total;                       // classes, workgroups
+  NsClass c[kNsClasses];
+};
+
+// elements of a slice
+inline int64_t ns_y_plane(int p, int lq) { return (int64_t)((p + kNsStep - 1) / kNsStep * kNsStep) * lq; }
+inline int64_t ns_s_plane(int p, int lp) { return (int64_t)p * lp; }
+
+struct MuonTables {                        // in the workspace, one row per matrix
+  MuonEntry* entries;
+  const MuonMat* mats;
+  double* partials;                        // kMuonParts per matrix
+  int* info;                               // 1: a non-finite entry
+};
+
+// M = mu M + G and the partial sums of squares of B; copies the pointers and shapes of `count` matrices
+// (rows mat0 ..) into the tables.  entries[i].M null: B = G.
+hipError_t launch_muon_begin(const MuonEntry* entries, const MuonMat* mats, int mat0, int count, const MuonTables& t, float mu,
+                             bool nesterov, bool g_bf16, hipStream_t st);
+// Y = B * (scale / (||B||_F + eps)) in fp16 words, zero padding, info words
+hipError_t launch_muon_scale(const NsArgs& a, const MuonTables& t, float mu, bool nesterov, bool g_bf16, int parts, double eps,
+                             double scale, hipStream_t st);
+// S = out_scale * Y Y^T of Y buffer `src`
+hipError_t launch_ns_gram(const NsArgs& a, int parts, int src, float out_scale, hipStream_t st);
+// P = out_scale * (a I + b S + c S S); the stored S is S * s_scale
+hipError_t launch_ns_poly(const NsArgs& a, int parts, float ca, float cb, float cc, float s_scale, float out_scale, hipStream_t st);
+// Y' = out_scale * P Y, from Y buffer `src` to the other one
+hipError_t launch_ns_apply(const NsArgs& a, int parts, int src, float out_scale, hipStream_t st);
+// O = out_scale * P Y; X = O, or with `update` X = keep X - lr scale_i O
+hipError_t launch_ns_final(const NsArgs& a, const MuonTables& t, int parts, int src, float out_scale, bool update, float keep, float lr,
+                           bool x_bf16, hipStream_t st);
+
+}  // namespace od

@@ -1,0 +1,292 @@
+"""Muon on the GPU against the fp64 oracle: sizes and strides where tiles, steps and padding end, types and precisions, sets
+of many shapes, matrices that are zero, tiny, huge or not finite, streams and captured graphs.
+
+Tolerance of O, derived before the first run.  Operands are rounded to u (half a step: 2^-11 with fp16 words, 2^-22 with two of
+them, and the fp32 sums add 2^-24 sqrt(K / 16) of a product's size).  Step k rounds three of them (Y, S, P), each a relative error of
+at most u in the Frobenius norm of X_k; an error in the plane of two singular vectors is multiplied by the later steps as X's own
+singular values are, by prod |a + b s^2 + c s^4|, or along one by the derivative.  Errors spread over all directions alike, so the
+root mean square of that factor over the spectrum counts.  u is the largest error of a rounding and its root mean square
+0.4 u, which leaves room for the part of it that is not spread evenly."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle.optimizers_oracle import muon_step, newton_schulz, newton_schulz_path
+from paper_2605_16341_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+QUINTIC = binding.MUON_COEFFS
+HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
+
+def tolerance(a, coeffs, exact, out):
+    path = newton_schulz_path(a, coeffs)
+    u = 2.0 ** -11 if not exact else 2.0 ** -22 + 2.0 ** -24 * (1 + math.sqrt(max(a.shape) / 16))
+    s = np.linalg.svd(path[0], compute_uv=False)
+    values = [s]
+    for ca, cb, cc in coeffs:
+        s = ca * s + cb * s ** 3 + cc * s ** 5
+        values.append(s)
+    total, grow, slope = 0.0, np.ones_like(s), np.ones_like(s)
+    for k in range(len(coeffs) - 1, -1, -1):
+        ca, cb, cc = coeffs[k]
+        v = values[k]
+        # rounding of S, P and of the Y that step k read
+        grow = grow * np.abs(ca + cb * v ** 2 + cc * v ** 4)
+        slope = slope * np.abs(ca + 3 * cb * v ** 2 + 5 * cc * v ** 4)
+        total += 3 * u * np.linalg.norm(path[k]) * math.sqrt(np.mean(np.maximum(grow, slope) ** 2))
+    return total / np.linalg.norm(path[-1]) + HALF[out]
+
+
+def types(torch, name):
+    return {"bf16": torch.bfloat16, "f32": torch.float32}[name]
+
+
+def matrix(rng, m, n, kind="noise"):
+    a = rng.standard_normal((m, n))
+    if kind == "spiked":                       # one large singular value over a floor
+        a = 10 * np.outer(rng.standard_normal(m), rng.standard_normal(n)) + a
+    if kind == "holes":                        # zero rows and columns
+        a[m // 2] = 0
+        a[:, n // 3] = 0
+    return 1e-2 * a
+
+
+def upload(torch, a, dtype, ld=None, offset=0):
+    """The matrix on the device with rows `ld` elements apart, starting `offset` elements into its buffer; the buffer
+    around it is filled with 7."""
+    m, n = a.shape
+    ld = ld or n
+    buf = torch.full((offset + m * ld + 8,), 7.0, device="cuda:0", dtype=dtype)
+    view = buf[offset:offset + m * ld].view(m, ld)[:, :n]
+    view.copy_(torch.from_numpy(a))
+    return buf, view
+
+
+def untouched(torch, buf, view, ld, offset):
+    m, n = view.shape
+    keep = torch.ones_like(buf, dtype=torch.bool)
+    keep[offset:offset + m * ld].view(m, ld)[:, :n] = False
+    return bool((buf[keep] == 7.0).all())
+
+
+def check(got, want, tol):
+    got = got.double().cpu().numpy()
+    err = np.linalg.norm(got - want) / max(np.linalg.norm(want), 1e-300)
+    assert err <= tol, (err, tol)
+    rms = np.linalg.norm(want) / math.sqrt(want.size)
+    worst = np.max(np.abs(got - want) / np.maximum(np.abs(want), rms))
+    assert worst <= 8 * tol, (worst, tol)
+
+
+SHAPES = [(1, 1), (1, 7), (5, 1), (3, 3), (2, 300), (300, 2), (8, 64), (64, 64), (65, 63), (127, 129), (129, 127), (128, 256),
+          (200, 328), (130, 1000), (1000, 130), (257, 513), (640, 384), (31, 2500), (512, 4104)]
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("x,g,precision", [("bf16", "bf16", "auto"), ("f32", "f32", "auto"), ("f32", "bf16", "fast"), ("bf16", "f32", "auto")])
+def test_orthogonalise(shape, x, g, precision):
+    import torch
+    rng = np.random.default_rng(shape[0] * 1000 + shape[1])
+    opt = binding.Muon([shape], x_dtype=x, g_dtype=g, precision=precision)
+    _, a = upload(torch, matrix(rng, *shape), types(torch, g))
+    buf, o = upload(torch, np.zeros(shape), types(torch, x))
+    opt.orthogonalise([a], [o])
+    host = a.double().cpu().numpy()
+    exact = precision == "auto" and not (x == g == "bf16")
+    check(o, newton_schulz(host, QUINTIC), tolerance(host, QUINTIC, exact, x))
+    assert opt.info() == [0] and untouched(torch, buf, o, shape[1], 0)
+
+
+@pytest.mark.parametrize("kind", ["spiked", "holes"])
+@pytest.mark.parametrize("shape", [(96, 160), (300, 200)])
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+def test_orthogonalise_spectra(kind, shape, x):
+    import torch
+    opt = binding.Muon([shape], x_dtype=x)
+    _, a = upload(torch, matrix(np.random.default_rng(3), *shape, kind), types(torch, x))
+    _, o = upload(torch, np.zeros(shape), types(torch, x))
+    opt.orthogonalise([a], [o])
+    host = a.double().cpu().numpy()
+    check(o, newton_schulz(host, QUINTIC), tolerance(host, QUINTIC, x == "f32", x))
+    if kind == "holes":
+        assert bool((o[shape[0] // 2] == 0).all()) and bool((o[:, shape[1] // 3] == 0).all())
+
+
+@pytest.mark.parametrize("lds,offset", [((72, 80, 96), 0), ((71, 77, 79), 0), ((72, 80, 96), 3), ((67, 67, 67), 1)])
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(130, 67), (50, 67)])
+def test_step_strides_and_alignment(lds, offset, x, shape):
+    """Rows further apart than their length, odd strides, pointers off a 16-byte boundary; what lies between is left alone."""
+    import torch
+    rng = np.random.default_rng(4)
+    dt = types(torch, x)
+    opt = binding.Muon([shape], x_dtype=x, lr=0.1, weight_decay=0.5, mu=0.9, scale="rms", lds=[lds])
+    bx, X = upload(torch, rng.standard_normal(shape), dt, lds[0], offset)
+    bg, G = upload(torch, matrix(rng, *shape), dt, lds[1], offset)
+    bm, M = upload(torch, matrix(rng, *shape), torch.float32, lds[2], offset)
+    x0, g0, m0 = (t.double().cpu().numpy() for t in (X, G, M))
+    opt.step([X], [G], [M])
+    scale = 0.2 * math.sqrt(max(shape))
+    wx, wm, wo = muon_step(x0, g0, m0, QUINTIC, 0.9, 0.1, 0.5, scale)
+    assert np.allclose(M.double().cpu().numpy(), wm, rtol=2.0 ** -22, atol=2.0 ** -22 * np.abs(wm).max())
+    tol = tolerance(g0 + 0.9 * wm, QUINTIC, x == "f32", "f32")
+    room = 0.1 * scale * tol * np.linalg.norm(wo) + 3 * HALF[x] * np.linalg.norm(wx)
+    check(X, wx, room / np.linalg.norm(wx))
+    assert untouched(torch, bx, X, lds[0], offset) and untouched(torch, bm, M, lds[2], offset) and untouched(torch, bg, G, lds[1], offset)
+
+
+@pytest.mark.parametrize("nesterov", [True, False])
+@pytest.mark.parametrize("x,g", [("bf16", "bf16"), ("f32", "f32"), ("f32", "bf16")])
+def test_three_steps_of_a_mixed_set(nesterov, x, g):
+    """More shapes than share a launch, several matrices of one shape, wide, tall and single rows, three steps on the same
+    state; every step starts from what the GPU left."""
+    import torch
+    rng = np.random.default_rng(5)
+    shapes = [(8 + 5 * i, 90 - 4 * i) for i in range(20)] + [(64, 96)] * 50 + [(1, 33), (33, 1), (200, 130), (130, 200)]
+    opt = binding.Muon(shapes, x_dtype=x, g_dtype=g, lr=0.05, weight_decay=0.1, mu=0.8, nesterov=nesterov)
+    X = [upload(torch, rng.standard_normal(s), types(torch, x))[1] for s in shapes]
+    M = [upload(torch, np.zeros(s), torch.float32)[1] for s in shapes]
+    for step in range(3):
+        G = [upload(torch, matrix(rng, *s), types(torch, g))[1] for s in shapes]
+        before = [[t.double().cpu().numpy() for t in seq] for seq in (X, G, M)]
+        opt.step(X, G, M)
+        assert opt.info() == [0] * len(shapes)
+        for i, s in enumerate(shapes):
+            scale = math.sqrt(max(1.0, s[0] / s[1]))
+            wx, wm, wo = muon_step(before[0][i], before[1][i], before[2][i], QUINTIC, 0.8, 0.05, 0.1, scale, nesterov)
+            assert np.allclose(M[i].double().cpu().numpy(), wm, rtol=2.0 ** -22, atol=2.0 ** -22 * np.abs(wm).max())
+            b = before[1][i] + 0.8 * wm if nesterov else wm
+            tol = tolerance(b, QUINTIC, not (x == g == "bf16"), "f32")
+            room = 0.05 * scale * tol * np.linalg.norm(wo) + 3 * HALF[x] * np.linalg.norm(wx)
+            check(X[i], wx, room / np.linalg.norm(wx))
+
+
+def test_zero_tiny_huge_and_non_finite_matrices_leave_the_others_alone():
+    import torch
+    rng = np.random.default_rng(6)
+    shape = (40, 56)
+    base = rng.standard_normal(shape)
+    nan, inf = base.copy(), base.copy()
+    nan[39, 55] = np.nan
+    inf[0, 0] = -np.inf
+    inputs = [base, 0 * base, 1e-38 * base, 1e-30 * base, 1e37 * base, nan, inf, base]
+    opt = binding.Muon([shape] * len(inputs), x_dtype="f32", eps=0.0)
+    A = [upload(torch, a, torch.float32)[1] for a in inputs]
+    O = [upload(torch, 0 * base, torch.float32)[1] for _ in inputs]
+    opt.orthogonalise(A, O)
+    assert opt.info() == [0, 0, 0, 0, 0, 1, 1, 0]
+    for k in (0, 2, 3, 4, 7):
+        host = A[k].double().cpu().numpy()
+        check(O[k], newton_schulz(host, QUINTIC, 0.0), tolerance(host / np.abs(host).max(), QUINTIC, True, "f32"))
+    assert bool((O[1] == 0).all()) and bool(O[5].isnan().all()) and bool(O[6].isnan().all())
+    assert torch.equal(O[0], O[7])
+    alone = binding.Muon([shape], x_dtype="f32", eps=0.0)
+    alone.orthogonalise([A[0]], [O[1]])
+    assert torch.equal(O[0], O[1])               # a matrix's bits do not depend on what is beside it
+
+
+def test_eps_damps_small_matrices():
+    import torch
+    a = matrix(np.random.default_rng(7), 30, 40)
+    opt = binding.Muon([a.shape], x_dtype="f32", eps=1.0)
+    _, A = upload(torch, a, torch.float32)
+    _, O = upload(torch, 0 * a, torch.float32)
+    opt.orthogonalise([A], [O])
+    host = A.double().cpu().numpy()
+    want = newton_schulz(host, QUINTIC, 1.0)
+    check(O, want, tolerance(host, QUINTIC, True, "f32"))
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+def test_converging_coefficients_give_orthonormal_rows(x):
+    """(15 s - 10 s^3 + 3 s^5) / 8 converges to 1: the rows of O are orthonormal up to the rounding of its last step."""
+    import torch
+    a = matrix(np.random.default_rng(8), 72, 320)
+    coeffs = ((1.875, -1.25, 0.375),) * 14
+    opt = binding.Muon([a.shape], x_dtype="f32", precision="fast" if x == "bf16" else "exact", coeffs=coeffs)
+    _, A = upload(torch, a, torch.float32)
+    _, O = upload(torch, 0 * a, torch.float32)
+    opt.orthogonalise([A], [O])
+    o = O.double().cpu().numpy()
+    # P's diagonal is rounded like an operand and scales whole rows: 2 u, and the sums of 72 and 320 products of rounded operands
+    u = 2.0 ** -11 if x == "bf16" else 2.0 ** -22 + 2.0 ** -24 * math.sqrt(320 / 16)
+    assert np.max(np.abs(o @ o.T - np.eye(72))) <= 8 * u
+
+
+def test_captured_steps_replay_and_share_a_workspace():
+    """Two handles on one workspace, captured into two graphs that are replayed in turn with eager work between them."""
+    import torch
+    rng = np.random.default_rng(9)
+    sets = [[(72, 130), (130, 72)], [(200, 96)]]
+    opts = [binding.Muon(s, x_dtype="bf16", lr=0.05, weight_decay=0.1) for s in sets]
+    need = max(o.workspace_bytes for o in opts)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda:0")
+    for o in opts:
+        o.workspace, o.workspace_bytes = ws, need
+
+    def state(seed):
+        r = np.random.default_rng(seed)
+        return [[[upload(torch, matrix(r, *s), dt)[1] for s in shapes] for dt in (torch.bfloat16, torch.bfloat16, torch.float32)]
+                for shapes in sets]
+
+    eager, graphed = state(1), state(1)
+    stream = torch.cuda.Stream()
+    graphs = []
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        for o, s in zip(opts, graphed):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=stream):
+                o.step(*s)
+            graphs.append(g)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for e, g in zip(eager, graphed) for x, y in zip(e, g) for a, b in zip(x, y))     # nothing ran
+    for turn in range(4):
+        for k in (0, 1):
+            fresh = [matrix(rng, *s) for s in sets[k]]
+            for j, f in enumerate(fresh):
+                eager[k][1][j].copy_(torch.from_numpy(f))
+                graphed[k][1][j].copy_(torch.from_numpy(f))
+            graphs[k].replay()
+            torch.cuda.synchronize()
+            opts[k].step(*eager[k])
+            torch.cuda.synchronize()
+            for a, b in zip(eager[k], graphed[k]):
+                assert all(torch.equal(x, y) for x, y in zip(a, b)), (turn, k)
+
+
+def test_other_stream_and_repeated_calls_give_the_same_bits():
+    import torch
+    shapes = [(96, 200), (333, 150)]
+    opt = binding.Muon(shapes, x_dtype="f32")
+    A = [upload(torch, matrix(np.random.default_rng(10), *s), torch.float32)[1] for s in shapes]
+    outs = []
+    for k in range(3):
+        O = [torch.empty_like(a) for a in A]
+        stream = torch.cuda.Stream() if k else torch.cuda.current_stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            opt.orthogonalise(A, O)
+        torch.cuda.synchronize()
+        outs.append(O)
+    assert all(torch.equal(a, b) for o in outs[1:] for a, b in zip(o, outs[0]))
+
+
+def test_parts_of_a_fused_projection():
+    """Query, key and value as column blocks of one matrix are three matrices of their own."""
+    import torch
+    m, n = 72, 88
+    full = matrix(np.random.default_rng(11), m, 3 * n)
+    _, G = upload(torch, full, torch.bfloat16)
+    X = torch.zeros(m, 3 * n, device="cuda:0", dtype=torch.bfloat16)
+    opt = binding.Muon([(m, n)] * 3, x_dtype="bf16", lds=[(3 * n,) * 3] * 3)
+    cut = lambda t: [t[:, k * n:(k + 1) * n] for k in range(3)]
+    opt.orthogonalise(cut(G), cut(X))
+    for a, o in zip(cut(G), cut(X)):
+        host = a.double().cpu().numpy()
+        check(o, newton_schulz(host, QUINTIC), tolerance(host, QUINTIC, False, "bf16"))
+    with pytest.raises(ValueError):
+        opt.orthogonalise([t.contiguous() for t in cut(G)], cut(X))
