@@ -4,8 +4,8 @@
 // A matrix A (m x n) is worked on as Y (p x q) with p = min(m, n), q = max(m, n): A itself or its transpose.
 // Its slice of the workspace holds fp16 operand words only, `parts` planes (1: the value under a power-of-two
 // scale, 2: hi + lo of it) of
-//   Y twice (read by one iteration, written for the next)   pp rows of lq, rows p .. pp and columns q .. qq zero
-//   S = Y Y^T and P = a I + b S + c S S                     p rows of lp, columns p .. pp zero
+//   Y twice (read by one product, written by another)   pp rows of lq, rows p .. pp and columns q .. qq zero
+//   symmetric p x p matrices                             p rows of lp, columns p .. pp zero
 // with pp and qq the multiples of 64 above p and q: the K loops run over whole 64-deep steps unchecked.
 #pragma once
 
@@ -15,7 +15,8 @@
 namespace od {
 
 constexpr int kNsStep = 64;                // k of one step of the K loops
-constexpr int kNsClasses = 16;             // classes (matrices of one shape) that share a launch
+constexpr int kNsClasses = 16;             // classes (matrices of one shape) that step together
+constexpr int kNsJobs = 2 * kNsClasses;    // jobs of one launch: up to two per class
 constexpr int kMuonChunk = 48;             // matrices whose pointers travel in one launch's arguments
 constexpr int kMuonParts = 256;            // most partial sums of squares of one matrix
 
@@ -33,19 +34,27 @@ struct MuonMat {                           // one matrix, as the elementwise ker
   int blocks;                              // partial sums
 };
 
-// One class in a launch over several: nb matrices of p x q (or q x p where tall).
-struct NsClass {
-  int first;                               // first workgroup of the class
+// What a launch computes for one class: nb matrices of p x q (or q x p where tall).
+enum NsKind : int {
+  NS_GRAM = 0,                             // out = cc a a^T of Y at a
+  NS_SYM = 1,                              // out = ca I + cb e + cc a b of commuting symmetric a, b; e read where cb != 0
+  NS_APPLY = 2                             // out = cc a b of symmetric a and Y at b
+};
+struct NsJob {
+  int first;                               // first workgroup of the job
   int p, q, lp, lq, nb;
   int mat0;                                // first row of the class in the matrix tables
   int tall;
-  uint16_t* base;                          // slice of its first matrix
+  uint16_t* base;                          // slice of the class's first matrix
   int64_t stride;                          // elements between slices
+  int64_t a, b, e, out;                    // operands in a slice, elements
+  float ca, cb, cc;
+  int kind;
 };
 
 struct NsArgs {
-  int nclass, total;                       // classes, workgroups
-  NsClass c[kNsClasses];
+  int count, total;                        // jobs, workgroups
+  NsJob j[kNsJobs];
 };
 
 // elements of a slice
@@ -63,17 +72,12 @@ struct MuonTables {                        // in the workspace, one row per matr
 // (rows mat0 ..) into the tables.  entries[i].M null: B = G.
 hipError_t launch_muon_begin(const MuonEntry* entries, const MuonMat* mats, int mat0, int count, const MuonTables& t, float mu,
                              bool nesterov, bool g_bf16, hipStream_t st);
-// Y = B * (scale / (||B||_F + eps)) in fp16 words, zero padding, info words
+// Y = B * (scale / (||B||_F + eps)) in fp16 words, zero padding, info words; one job per class
 hipError_t launch_muon_scale(const NsArgs& a, const MuonTables& t, float mu, bool nesterov, bool g_bf16, int parts, double eps,
                              double scale, hipStream_t st);
-// S = out_scale * Y Y^T of Y buffer `src`
-hipError_t launch_ns_gram(const NsArgs& a, int parts, int src, float out_scale, hipStream_t st);
-// P = out_scale * (a I + b S + c S S); the stored S is S * s_scale
-hipError_t launch_ns_poly(const NsArgs& a, int parts, float ca, float cb, float cc, float s_scale, float out_scale, hipStream_t st);
-// Y' = out_scale * P Y, from Y buffer `src` to the other one
-hipError_t launch_ns_apply(const NsArgs& a, int parts, int src, float out_scale, hipStream_t st);
-// O = out_scale * P Y; X = O, or with `update` X = keep X - lr scale_i O
-hipError_t launch_ns_final(const NsArgs& a, const MuonTables& t, int parts, int src, float out_scale, bool update, float keep, float lr,
-                           bool x_bf16, hipStream_t st);
+// the products of the jobs
+hipError_t launch_ns_products(const NsArgs& a, int parts, hipStream_t st);
+// O = cc a b of jobs of kind NS_APPLY, into the callers' matrices: X = O, or with `update` X = keep X - lr scale_i O
+hipError_t launch_ns_final(const NsArgs& a, const MuonTables& t, int parts, bool update, float keep, float lr, bool x_bf16, hipStream_t st);
 
 }  // namespace od

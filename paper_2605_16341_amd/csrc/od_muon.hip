@@ -4,9 +4,13 @@
 //   X0 = B / (||B||_F + eps)
 //   S  = Xk Xk^T,   P = a I + b S + c S S,   Xk+1 = P Xk        K times
 //   X  = (1 - lr wd) X - lr scale XK
-// S, S S and P are symmetric: only tiles on and above the diagonal are computed, the others mirrored.
-// See od_muon.h for the layout of the workspace.
+// S, S S and P are symmetric: only tiles on and above the diagonal are computed, the others mirrored.  All polynomials in
+// S commute, so several steps can share one S = Xk Xk^T and one product with Xk:
+//   Z = P,  then per further step  S = P S P,  P = a I + b S + c S S,  Z = P Z,  and at last  Xk+L = Z Xk
+// (which steps do is the host's plan).  See od_muon.h for the layout of the workspace.
 #include "od_muon.h"
+
+#include <type_traits>
 
 #include "od_dma.h"
 
@@ -131,11 +135,15 @@ OD_DEV void split2(float a, float b, uint32_t* out) {
   }
 }
 
-OD_DEV int ns_class(const NsArgs& a, int bid) {
+OD_DEV int ns_job(const NsArgs& a, int bid) {
   int k = 0;
-  while (k + 1 < a.nclass && bid >= a.c[k + 1].first) ++k;
+  while (k + 1 < a.count && bid >= a.j[k + 1].first) ++k;
   return k;
 }
+
+// Uniform integer division runs on the vector units; this brings its results back to scalar registers, where addresses
+// and loop counts belong.
+OD_DEV int quotient(int a, int b) { return __builtin_amdgcn_readfirstlane(a / b); }
 
 OD_DEV int up64(int v) { return (v + 63) & ~63; }
 
@@ -144,7 +152,7 @@ template <bool GBF, int PARTS>
 __global__ __launch_bounds__(256) void k_muon_scale(NsArgs args, MuonTables t, float mu, int nesterov, double eps, double scale) {
   __shared__ double lds[4];
   __shared__ float tile[64][65];
-  const NsClass c = args.c[ns_class(args, blockIdx.x)];
+  const NsJob c = args.j[ns_job(args, blockIdx.x)];
   const int pp = up64(c.p), qq = up64(c.q), ti_n = pp / 64, tj_n = qq / 64;
   const int in_class = blockIdx.x - c.first, z = in_class / (ti_n * tj_n), tl = in_class % (ti_n * tj_n);
   const int ti = tl / tj_n, tj = tl % tj_n;
@@ -223,16 +231,27 @@ __global__ __launch_bounds__(256) void k_muon_scale(NsArgs args, MuonTables t, f
 // ------------------------------------------------------------------------------------
 // The products.  One workgroup computes a T x T tile of C = A B over 64-deep steps; A has k along its rows, B is given
 // either as the rows of B^T with k along them (TRB = false) or as rows of B, k down its columns (TRB = true).  Both
-// operands come by direct-to-LDS loads into two stages:
+// operands come by direct-to-LDS loads into a ring of five operand tiles (A0 B0 A1 B1 A2 ..):
 //   k along rows   128-byte rows, their 16-byte k-groups XOR-swizzled by (row >> 1) & 7: the 16 lanes that a
 //                  ds_read_b128 serves at a time lie in 16 different groups of four banks
 //   k down columns rows of T elements, their 64-byte blocks XOR-swizzled by k & 3, so that the four rows of a
 //                  ds_read_b64_tr_b16 lie in different banks
 // With two parts a product is three passes over K: hi hi, hi lo, lo hi.
 // ------------------------------------------------------------------------------------
-OD_DEV void dma16_at(uint32_t voff, const void* sbase, uint32_t lds_base) {
-  const uint32_t l = __builtin_amdgcn_readfirstlane(lds_base);
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n" ::"v"(voff), "s"(sbase), "s"(l) : "memory");
+// As dma16, from a uniform base plus 32-bit lane offsets; all lanes of the wave are active, and `mask` (all ones or zero)
+// takes the load away without a branch, past which accumulators would be moved about.
+OD_DEV void dma16_at(uint32_t voff, const void* sbase, uint32_t lds_base, uint32_t mask) {
+  const uint32_t l = __builtin_amdgcn_readfirstlane(lds_base), m = __builtin_amdgcn_readfirstlane(mask);
+  asm volatile("s_mov_b32 m0, %2\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1\n" ::"v"(voff), "s"(sbase), "s"(l), "s"(m) : "memory");
+}
+
+// f(0), f(1), .. f(N - 1) with the index a constant, so that register arrays stay registers
+template <int N, int I = 0, class F>
+OD_DEV void static_for(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    static_for<N, I + 1>(f);
+  }
 }
 
 OD_DEV int swz64(int row) { return (row >> 1) & 7; }
@@ -248,9 +267,9 @@ template <int T_, int WI_, int WJ_>
 struct NsTile {
   static constexpr int T = T_, WI = WI_, WJ = WJ_, NW = WI * WJ, THREADS = 64 * NW;
   static constexpr int WTM = T / WI, WTN = T / WJ, FM = WTM / 32, FN = WTN / 32;
-  static constexpr int OPER = T * 128, STAGE = 2 * OPER, LDS = 2 * STAGE;   // bytes
-  static constexpr int CH = T / 8 / NW;                                       // 1 KB loads per wave, stage and operand
-  static_assert(NW * WTM * WTN * 2 <= LDS, "the waves' tiles are staged in LDS");
+  static constexpr int OPER = T * 128, RING = 5, LDS = RING * OPER;          // bytes of a tile's operand step, ring
+  static constexpr int BLOCKS = T == 128 ? 2 : 1;                             // workgroups per CU
+  static constexpr int CH = T / 8 / NW;                                       // 1 KB loads per wave and operand tile
 };
 
 // ACROSS: the accumulator of lane l holds C[l % 32][4 consecutive columns], otherwise C[4 consecutive rows][l % 32]
@@ -277,15 +296,21 @@ OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const 
   }
   const int ks = kdim / kNsStep, steps = ks * (PARTS == 2 ? 3 : 1);
   const int64_t bstep = TRB ? (int64_t)kNsStep * B.ld : kNsStep;
-  auto issue = [&](int step) {
-    const int seg = PARTS == 2 ? step / ks : 0, kk = PARTS == 2 ? step - seg * ks : step;
-    const uint16_t* a = A.p + (seg == 2 ? A.plane : 0) + (int64_t)kk * kNsStep;
-    const uint16_t* b = B.p + (seg == 1 ? B.plane : 0) + kk * bstep;
-    const uint32_t at = lds0 + (step & 1) * TL::STAGE + wave * CH * 1024;
-#pragma unroll
-    for (int j = 0; j < CH; ++j) dma16_at(va[j], a, at + j * 1024);
-#pragma unroll
-    for (int j = 0; j < CH; ++j) dma16_at(vb[j], b, at + TL::OPER + j * 1024);
+  // loads of one operand tile of one step; of a step past the last one, none
+  struct Loads { const uint16_t* p; uint32_t at, mask; };
+  auto slot = [&](int unit) { return (uint32_t)(unit % TL::RING) * TL::OPER; };
+  auto loads_of = [&](int step, bool of_b) {
+    const int seg = PARTS == 2 ? quotient(step, ks) : 0, kk = PARTS == 2 ? step - seg * ks : step;
+    const uint16_t* p = of_b ? B.p + (seg == 1 ? B.plane : 0) + kk * bstep : A.p + (seg == 2 ? A.plane : 0) + (int64_t)kk * kNsStep;
+    return Loads{p, lds0 + slot(2 * step + of_b) + wave * CH * 1024, step < steps ? ~0u : 0u};
+  };
+  auto issue_a = [&](const Loads& l, auto jj) {
+    constexpr int j = decltype(jj)::value;
+    dma16_at(va[j], l.p, l.at + j * 1024, l.mask);
+  };
+  auto issue_b = [&](const Loads& l, auto jj) {
+    constexpr int j = decltype(jj)::value;
+    dma16_at(vb[j], l.p, l.at + j * 1024, l.mask);
   };
 #pragma unroll
   for (int i = 0; i < TL::FM; ++i)
@@ -295,13 +320,15 @@ OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const 
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
   u32x4 fa[2][TL::FM], fb[2][TL::FN];
-  auto fetch = [&](int step, int sub, int set) {
-    const char* base = lds + (step & 1) * TL::STAGE;
+  auto fetch = [&](int step, int sub, auto ss) {
+    constexpr int set = decltype(ss)::value;
+    const char* at_a = lds + slot(2 * step);
+    const char* at_b = lds + slot(2 * step + 1);
     const int kg = 2 * sub + (lane >> 5);
 #pragma unroll
     for (int i = 0; i < TL::FM; ++i) {
       const int row = wi * TL::WTM + 32 * i + (lane & 31);
-      fa[set][i] = *reinterpret_cast<const u32x4*>(base + row * 128 + ((kg ^ swz64(row)) << 4));
+      fa[set][i] = *reinterpret_cast<const u32x4*>(at_a + row * 128 + ((kg ^ swz64(row)) << 4));
     }
 #pragma unroll
     for (int j = 0; j < TL::FN; ++j) {
@@ -310,138 +337,143 @@ OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const 
         const int col = wj * TL::WTN + 32 * j + ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
         const int at = k * (2 * T) + (((col >> 3) ^ ((k & 3) << 2)) << 4) + (col & 7) * 2;
         typedef __attribute__((address_space(3))) s16x4* lptr;
-        const char* p = base + TL::OPER + at;
+        const char* p = at_b + at;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(p));
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(p + 4 * (2 * T)));
         const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
         fb[set][j] = u32x4{l2[0], l2[1], h2[0], h2[1]};
       } else {
         const int row = wj * TL::WTN + 32 * j + (lane & 31);
-        fb[set][j] = *reinterpret_cast<const u32x4*>(base + TL::OPER + row * 128 + ((kg ^ swz64(row)) << 4));
+        fb[set][j] = *reinterpret_cast<const u32x4*>(at_b + row * 128 + ((kg ^ swz64(row)) << 4));
       }
     }
   };
-  auto products = [&](int set) {
-#pragma unroll
-    for (int i = 0; i < TL::FM; ++i)
-#pragma unroll
-      for (int j = 0; j < TL::FN; ++j)
-        acc[i][j] = ACROSS ? mfma_32x32x16<true>(fb[set][j], fa[set][i], acc[i][j])
-                           : mfma_32x32x16<true>(fa[set][i], fb[set][j], acc[i][j]);
+  auto product = [&](auto ii, auto jj, auto ss) {
+    constexpr int i = decltype(ii)::value, j = decltype(jj)::value, set = decltype(ss)::value;
+    acc[i][j] = ACROSS ? mfma_32x32x16<true>(fb[set][j], fa[set][i], acc[i][j])
+                       : mfma_32x32x16<true>(fa[set][i], fb[set][j], acc[i][j]);
   };
+  // the products of one quarter of a step with `count` loads, from `first` on, spread between them: issued in a row they
+  // would hold the wave up until the memory path took them all
+  auto products = [&](auto ss, auto first, auto count, auto&& load) {
+    constexpr int N = TL::FM * TL::FN, F = decltype(first)::value, C = decltype(count)::value;
+    static_for<N>([&](auto mm) {
+      constexpr int m = decltype(mm)::value, before = m * C / N, after = (m + 1) * C / N;
+      product(std::integral_constant<int, m / TL::FN>{}, std::integral_constant<int, m % TL::FN>{}, ss);
+      if constexpr (after > before) {
+        __builtin_amdgcn_sched_barrier(0);
+        static_for<after - before>([&](auto k) { load(std::integral_constant<int, F + before + decltype(k)::value>{}); });
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    });
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  constexpr std::integral_constant<int, 0> even{};
+  constexpr std::integral_constant<int, 1> odd{};
 
-  // Stage i + 1 is in flight during step i.  The last quarter of a step is multiplied from registers after the barrier
-  // that frees its stage, so the first operands of the next step arrive behind products, not in front of them.
-  issue(0);
-  if (steps > 1) {
-    issue(1);
-    __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * CH));
-  } else {
-    __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
-  }
+  // Step i multiplies quarters 0 .. 3 of A(i), B(i), each from registers that were read during the quarter before.  The last
+  // quarter comes behind the barrier that frees the tiles of step i and admits those of step i + 1, so no product
+  // waits for the first operands of a step.  B(i + 2) is loaded right behind that barrier, A(i + 3) during the following
+  // three quarters: the loads are spread over the step, and the ones issued late have a step more to arrive.
+  constexpr int C0 = (CH + 1) / 2, C1 = (CH - C0 + 1) / 2, C2 = CH - C0 - C1;
+  static_for<4>([&](auto u) {
+    const Loads l = loads_of(decltype(u)::value / 2, decltype(u)::value % 2);
+    static_for<CH>([&](auto j) {
+      if constexpr (decltype(u)::value % 2) issue_b(l, j);
+      else issue_a(l, j);
+    });
+  });
+  __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * CH));
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  fetch(0, 0, 0);
+  fetch(0, 0, even);
   for (int i = 0; i < steps; ++i) {
-    fetch(i, 1, 1);
-    products(0);
-    fetch(i, 2, 0);
-    products(1);
-    fetch(i, 3, 1);
-    products(0);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    const Loads la = loads_of(i + 2, false), lb = loads_of(i + 2, true);
+    auto from_a = [&](auto j) { issue_a(la, j); };
+    fetch(i, 1, odd);
+    __builtin_amdgcn_sched_barrier(0);
+    products(even, std::integral_constant<int, 0>{}, std::integral_constant<int, C0>{}, from_a);
+    fetch(i, 2, even);
+    __builtin_amdgcn_sched_barrier(0);
+    products(odd, std::integral_constant<int, C0>{}, std::integral_constant<int, C1>{}, from_a);
+    fetch(i, 3, odd);
+    __builtin_amdgcn_sched_barrier(0);
+    products(even, std::integral_constant<int, C0 + C1>{}, std::integral_constant<int, C2>{}, from_a);
+    // this wave's reads of step i are done, and all its loads but those of A(i + 2)
+    __builtin_amdgcn_s_waitcnt(vmcnt_only(CH));
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (i + 2 < steps) issue(i + 2);
-    if (i + 1 < steps) fetch(i + 1, 0, 0);
-    products(1);
+    fetch(i + 1, 0, even);                 // past the last step: what lies there, never used
+    __builtin_amdgcn_sched_barrier(0);
+    products(odd, std::integral_constant<int, 0>{}, std::integral_constant<int, CH>{}, [&](auto j) { issue_b(lb, j); });
   }
+  __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
 }
 
-// Writes a wave's tile of fp16 words (value * scale) row by row through its own part of LDS, 16 bytes a lane, and with
-// `mirror` the transpose too.  `value(row, col, v)`: the value whose accumulator entry is v, row and column in the
-// wave's tile.  Rows up to `rows` and columns up to `cols` of the matrix are written, from `crows` / `ccols` on as zero.
+// Writes a wave's tile of fp16 words 16 bytes a lane, with `mirror` the transpose too: 32 rows at a time through the
+// wave's own part of LDS.  `value(i, j, v4, row, col, x)`: the four values of accumulator (i, j) from entry 4 v4 on, the
+// first of them at row, col of the wave's tile.  Rows below `rows` and columns below `cols` are written, from `valid` on as zero.
 template <class TL, int PARTS, class V>
 OD_DEV void ns_store(char* lds, V&& value, uint16_t* out, int64_t plane, int ld, int row0, int col0, int rows, int cols,
-                     int valid_cols, bool mirror) {
+                     int valid, bool mirror) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  constexpr int ROWB = TL::WTN * 2, SL = ROWB / 16;       // bytes and 16-byte slots of a staged row
-  static_assert(SL == 8, "a staged row is 128 bytes");
-  char* mine = lds + wave * (TL::WTM * ROWB);
-  // The words of all parts from one evaluation: evaluated once more for the second part, a value might be contracted
-  // differently, round to another first word near a tie and leave a remainder of that one.
-  u32x2 words[PARTS][TL::FM][TL::FN][4];
+  constexpr int ROWB = TL::WTN * 2, SL = ROWB / 16, PIECE = 32 * ROWB;       // bytes and 16-byte slots of a staged row
+  static_assert(TL::NW * PARTS * PIECE <= TL::LDS, "staging");
+  auto swz = [](int r) { return SL == 8 ? swz64(r) : r & (SL - 1); };
+  auto masked = [&](u32x4 w, int col) {
+    if (col + 8 > valid) {
 #pragma unroll
-  for (int i = 0; i < TL::FM; ++i)
-#pragma unroll
-    for (int j = 0; j < TL::FN; ++j)
-#pragma unroll
-      for (int v4 = 0; v4 < 4; ++v4) {
-        float x[4];
-        value(i, j, v4, 32 * i + (lane & 31), 32 * j + 8 * v4 + 4 * (lane >> 5), x);
-        uint32_t a[PARTS], b[PARTS];
-        split2<PARTS>(x[0], x[1], a);
-        split2<PARTS>(x[2], x[3], b);
-#pragma unroll
-        for (int part = 0; part < PARTS; ++part) words[part][i][j][v4] = u32x2{a[part], b[part]};
-      }
-#pragma unroll
-  for (int part = 0; part < PARTS; ++part) {
-#pragma unroll
-    for (int i = 0; i < TL::FM; ++i)
-#pragma unroll
-      for (int j = 0; j < TL::FN; ++j)
-#pragma unroll
-        for (int v4 = 0; v4 < 4; ++v4) {
-          const int r = 32 * i + (lane & 31), c = 32 * j + 8 * v4 + 4 * (lane >> 5);
-          *reinterpret_cast<u32x2*>(mine + r * ROWB + (((c >> 3) ^ swz64(r)) << 4) + (c & 7) * 2) = words[part][i][j][v4];
-        }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    uint16_t* o = out + part * plane;
-#pragma unroll
-    for (int it = 0; it < TL::WTM / 8; ++it) {
-      const int r = it * 8 + (lane >> 3), slot = lane & 7;
-      u32x4 w = *reinterpret_cast<const u32x4*>(mine + r * ROWB + ((slot ^ swz64(r)) << 4));
-      const int row = row0 + r, col = col0 + 8 * slot;
-      if (col + 8 > valid_cols) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t keep = (col + 2 * k < valid_cols ? 0xffffu : 0u) | (col + 2 * k + 1 < valid_cols ? 0xffff0000u : 0u);
-          w[k] &= keep;
-        }
-      }
-      if (row < rows && col < cols) *reinterpret_cast<u32x4*>(o + (int64_t)row * ld + col) = w;
+      for (int k = 0; k < 4; ++k) w[k] &= (col + 2 * k < valid ? 0xffffu : 0u) | (col + 2 * k + 1 < valid ? 0xffff0000u : 0u);
     }
-    if (mirror) {
-      // lane l receives rows 8 (l / 16) .. + 7 of column l % 16 of each block of 32 rows and 16 columns
-      typedef __attribute__((address_space(3))) s16x4* lptr;
+    return w;
+  };
+  char* mine = lds + wave * (PARTS * PIECE);
+  static_for<TL::FM>([&](auto ii) {
+    constexpr int i = decltype(ii)::value;
+    static_for<TL::FN * 4>([&](auto jj) {
+      constexpr int j = decltype(jj)::value / 4, v4 = decltype(jj)::value % 4;
+      const int r = lane & 31, c = 32 * j + 8 * v4 + 4 * (lane >> 5);
+      float x[4];
+      value(ii, std::integral_constant<int, j>{}, std::integral_constant<int, v4>{}, 32 * i + r, c, x);
+      // both parts from one evaluation: evaluated once more, a value might be contracted differently, round to another
+      // first word near a tie and leave a remainder of that one
+      uint32_t a[PARTS], b[PARTS];
+      split2<PARTS>(x[0], x[1], a);
+      split2<PARTS>(x[2], x[3], b);
 #pragma unroll
-      for (int rb = 0; rb < TL::WTM / 32; ++rb)
+      for (int part = 0; part < PARTS; ++part)
+        *reinterpret_cast<u32x2*>(mine + part * PIECE + r * ROWB + (((c >> 3) ^ swz(r)) << 4) + (c & 7) * 2) = u32x2{a[part], b[part]};
+    });
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) {
+      uint16_t* o = out + part * plane;
+      const char* piece = mine + part * PIECE;
+#pragma unroll
+      for (int it = 0; it < SL / 2; ++it) {
+        const int r = it * (64 / SL) + lane / SL, slot = lane % SL;
+        const u32x4 w = *reinterpret_cast<const u32x4*>(piece + r * ROWB + ((slot ^ swz(r)) << 4));
+        const int row = row0 + 32 * i + r, col = col0 + 8 * slot;
+        if (row < rows && col < cols) *reinterpret_cast<u32x4*>(o + (int64_t)row * ld + col) = masked(w, col);
+      }
+      if (mirror) {
+        // lane l receives rows 8 (l / 16) .. + 7 of column l % 16 of each block of 16 columns
+        typedef __attribute__((address_space(3))) s16x4* lptr;
 #pragma unroll
         for (int cb = 0; cb < TL::WTN / 16; ++cb) {
-          const int c = cb * 16 + 4 * (lane & 3);
-          s16x4 h[2];
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const int r = rb * 32 + (lane >> 4) * 8 + 4 * k + ((lane & 15) >> 2);
-            h[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(mine + r * ROWB + (((c >> 3) ^ swz64(r)) << 4) + (c & 7) * 2));
-          }
-          const u32x2 l2 = __builtin_bit_cast(u32x2, h[0]), h2 = __builtin_bit_cast(u32x2, h[1]);
-          u32x4 w{l2[0], l2[1], h2[0], h2[1]};
-          const int mrow = col0 + cb * 16 + (lane & 15), mcol = row0 + rb * 32 + (lane >> 4) * 8;
-          if (mcol + 8 > valid_cols) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t keep = (mcol + 2 * k < valid_cols ? 0xffffu : 0u) | (mcol + 2 * k + 1 < valid_cols ? 0xffff0000u : 0u);
-              w[k] &= keep;
-            }
-          }
-          if (mrow < rows && mcol < cols) *reinterpret_cast<u32x4*>(o + (int64_t)mrow * ld + mcol) = w;
+          const int c = cb * 16 + 4 * (lane & 3), r = (lane >> 4) * 8 + ((lane & 15) >> 2);
+          const s16x4 h0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(piece + r * ROWB + (((c >> 3) ^ swz(r)) << 4) + (c & 7) * 2));
+          const s16x4 h1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(piece + (r + 4) * ROWB + (((c >> 3) ^ swz(r + 4)) << 4) + (c & 7) * 2));
+          const u32x2 l2 = __builtin_bit_cast(u32x2, h0), h2 = __builtin_bit_cast(u32x2, h1);
+          const int row = col0 + cb * 16 + (lane & 15), col = row0 + 32 * i + (lane >> 4) * 8;
+          if (row < rows && col < cols) *reinterpret_cast<u32x4*>(o + (int64_t)row * ld + col) = masked(u32x4{l2[0], l2[1], h2[0], h2[1]}, col);
         }
+      }
     }
-    if (part + 1 < PARTS) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  });
 }
 
 // tile of the upper triangle: row i holds tiles i .. n - 1
@@ -455,43 +487,51 @@ OD_DEV void upper_tile(int t, int n, int* ti, int* tj) {
   *tj = i + t;
 }
 
-struct NsPoly {
-  float ca, cb, cc;       // of I, S and S S, with the scales of the stored words
-};
-
-// S = Y Y^T (POLY = false) or P = a I + b S + c S S (POLY = true)
-template <class TL, int PARTS, bool POLY>
-__global__ __launch_bounds__(TL::THREADS, 1) void k_ns_sym(NsArgs args, int src, NsPoly k) {
+// The jobs of one launch.
+template <class TL, int PARTS>
+__global__ __launch_bounds__(TL::THREADS, TL::BLOCKS) void k_ns_products(NsArgs args) {
   extern __shared__ __align__(16) char lds[];
   constexpr int T = TL::T;
   const int bid = xcd_contiguous(blockIdx.x, args.total);
-  const NsClass c = args.c[ns_class(args, bid)];
-  const int n = (c.p + T - 1) / T, per = n * (n + 1) / 2;
-  const int z = (bid - c.first) / per;
-  int ti, tj;
-  upper_tile((bid - c.first) - z * per, n, &ti, &tj);
-  const int pp = up64(c.p), qq = up64(c.q);
+  const NsJob c = args.j[ns_job(args, bid)];
+  const int pp = up64(c.p), qq = up64(c.q), ni = (c.p + T - 1) / T, local = bid - c.first;
   const int64_t yplane = (int64_t)pp * c.lq, splane = (int64_t)c.p * c.lp;
-  uint16_t* slice = c.base + z * c.stride;
-  uint16_t* S = slice + 2 * PARTS * yplane;
-  uint16_t* P = S + PARTS * splane;
-  const uint16_t* in = POLY ? S : slice + src * PARTS * yplane;
-  const int64_t plane = POLY ? splane : yplane;
-  const int ld = POLY ? c.lp : c.lq;
-  const NsOperand A{in + (int64_t)ti * T * ld, plane, ld, c.p - ti * T}, B{in + (int64_t)tj * T * ld, plane, ld, c.p - tj * T};
-  f32x16 acc[TL::FM][TL::FN];
-  ns_product<TL, PARTS, false, true>(acc, A, B, POLY ? pp : qq, lds);
-  __syncthreads();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row0 = ti * T + wave / TL::WJ * TL::WTM, col0 = tj * T + wave % TL::WJ * TL::WTN;
-  ns_store<TL, PARTS>(lds, [&](int i, int j, int v4, int r, int cl, float* x) {
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    const int row = row0 + r, col = col0 + cl;
-    if constexpr (POLY) {
-      if (row < c.p && col < pp) {
+  f32x16 acc[TL::FM][TL::FN];
+  if (c.kind == NS_APPLY) {
+    const int nj = (c.q + T - 1) / T;
+    const int z = quotient(local, ni * nj), tl = local - z * (ni * nj);
+    const int tj = quotient(tl, ni), ti = tl - tj * ni;
+    uint16_t* slice = c.base + z * c.stride;
+    const NsOperand A{slice + c.a + (int64_t)ti * T * c.lp, splane, c.lp, c.p - ti * T}, B{slice + c.b + tj * T, yplane, c.lq, qq - tj * T};
+    ns_product<TL, PARTS, true, true>(acc, A, B, pp, lds);
+    __syncthreads();
+    const int row0 = ti * T + wave / TL::WJ * TL::WTM, col0 = tj * T + wave % TL::WJ * TL::WTN;
+    ns_store<TL, PARTS>(lds, [&](auto i, auto j, auto v4, int, int, float* x) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = c.cc * acc[i][j][4 * v4 + e];
+    }, slice + c.out, yplane, c.lq, row0, col0, c.p, qq, c.q, false);
+  } else {
+    const int per = ni * (ni + 1) / 2;
+    const int z = quotient(local, per);
+    int ti, tj;
+    upper_tile(local - z * per, ni, &ti, &tj);
+    uint16_t* slice = c.base + z * c.stride;
+    const bool gram = c.kind == NS_GRAM;
+    const int64_t plane = gram ? yplane : splane;
+    const int ld = gram ? c.lq : c.lp;
+    const NsOperand A{slice + c.a + (int64_t)ti * T * ld, plane, ld, c.p - ti * T}, B{slice + c.b + (int64_t)tj * T * ld, plane, ld, c.p - tj * T};
+    ns_product<TL, PARTS, false, true>(acc, A, B, gram ? qq : pp, lds);
+    __syncthreads();
+    const int row0 = ti * T + wave / TL::WJ * TL::WTM, col0 = tj * T + wave % TL::WJ * TL::WTN;
+    const uint16_t* E = slice + c.e;
+    ns_store<TL, PARTS>(lds, [&](auto i, auto j, auto v4, int r, int cl, float* x) {
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+      const int row = row0 + r, col = col0 + cl;
+      if (c.cb != 0.f && row < c.p && col < pp) {
 #pragma unroll
         for (int part = 0; part < PARTS; ++part) {
-          const u32x2 w = *reinterpret_cast<const u32x2*>(S + part * splane + (int64_t)row * c.lp + col);
+          const u32x2 w = *reinterpret_cast<const u32x2*>(E + part * splane + (int64_t)row * c.lp + col);
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const uint32_t pair = w[e];          // a bit cast of a vector's element itself would take its first one
@@ -501,59 +541,26 @@ __global__ __launch_bounds__(TL::THREADS, 1) void k_ns_sym(NsArgs args, int src,
           }
         }
       }
-    }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[e] = k.cc * acc[i][j][4 * v4 + e];
-      if constexpr (POLY) x[e] += k.cb * s[e] + (row == col + e ? k.ca : 0.f);
-    }
-  }, POLY ? P : S, splane, c.lp, row0, col0, c.p, pp, c.p, ti != tj);
-}
-
-// Y' = P Y
-template <class TL, int PARTS>
-__global__ __launch_bounds__(TL::THREADS, 1) void k_ns_apply(NsArgs args, int src, float scale) {
-  extern __shared__ __align__(16) char lds[];
-  constexpr int T = TL::T;
-  const int bid = xcd_contiguous(blockIdx.x, args.total);
-  const NsClass c = args.c[ns_class(args, bid)];
-  const int ni = (c.p + T - 1) / T, nj = (c.q + T - 1) / T;
-  const int z = (bid - c.first) / (ni * nj), tl = (bid - c.first) - z * (ni * nj);
-  const int ti = tl % ni, tj = tl / ni;
-  const int pp = up64(c.p), qq = up64(c.q);
-  const int64_t yplane = (int64_t)pp * c.lq, splane = (int64_t)c.p * c.lp;
-  uint16_t* slice = c.base + z * c.stride;
-  const uint16_t* P = slice + 2 * PARTS * yplane + PARTS * splane;
-  const uint16_t* Y = slice + src * PARTS * yplane;
-  uint16_t* out = slice + (1 - src) * PARTS * yplane;
-  const NsOperand A{P + (int64_t)ti * T * c.lp, splane, c.lp, c.p - ti * T}, B{Y + tj * T, yplane, c.lq, qq - tj * T};
-  f32x16 acc[TL::FM][TL::FN];
-  ns_product<TL, PARTS, true, true>(acc, A, B, pp, lds);
-  __syncthreads();
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row0 = ti * T + wave / TL::WJ * TL::WTM, col0 = tj * T + wave % TL::WJ * TL::WTN;
-  ns_store<TL, PARTS>(lds, [&](int i, int j, int v4, int, int, float* x) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = scale * acc[i][j][4 * v4 + e];
-  }, out, yplane, c.lq, row0, col0, c.p, qq, c.q, false);
+      for (int e = 0; e < 4; ++e) x[e] = c.cc * acc[i][j][4 * v4 + e] + c.cb * s[e] + (row == col + e ? c.ca : 0.f);
+    }, slice + c.out, splane, c.lp, row0, col0, c.p, pp, c.p, ti != tj);
+  }
 }
 
 // O = P Y into the caller's matrix, or its update
 template <class TL, int PARTS, bool XBF, bool TALL>
-__global__ __launch_bounds__(TL::THREADS, 1) void k_ns_final(NsArgs args, MuonTables t, int src, float scale, int update, float keep, float lr) {
+__global__ __launch_bounds__(TL::THREADS, TL::BLOCKS) void k_ns_final(NsArgs args, MuonTables t, int update, float keep, float lr) {
   extern __shared__ __align__(16) char lds[];
   constexpr int T = TL::T;
   const int bid = xcd_contiguous(blockIdx.x, args.total);
-  const NsClass c = args.c[ns_class(args, bid)];
-  const int ni = (c.p + T - 1) / T, nj = (c.q + T - 1) / T;
-  const int z = (bid - c.first) / (ni * nj), tl = (bid - c.first) - z * (ni * nj);
-  const int ti = tl % ni, tj = tl / ni;
-  const int pp = up64(c.p), qq = up64(c.q);
+  const NsJob c = args.j[ns_job(args, bid)];
+  const float scale = c.cc;
+  const int pp = up64(c.p), qq = up64(c.q), ni = (c.p + T - 1) / T, nj = (c.q + T - 1) / T, local = bid - c.first;
   const int64_t yplane = (int64_t)pp * c.lq, splane = (int64_t)c.p * c.lp;
+  const int z = quotient(local, ni * nj), tl = local - z * (ni * nj);
+  const int tj = quotient(tl, ni), ti = tl - tj * ni;
   uint16_t* slice = c.base + z * c.stride;
-  const uint16_t* P = slice + 2 * PARTS * yplane + PARTS * splane;
-  const uint16_t* Y = slice + src * PARTS * yplane;
-  const NsOperand A{P + (int64_t)ti * T * c.lp, splane, c.lp, c.p - ti * T}, B{Y + tj * T, yplane, c.lq, qq - tj * T};
+  const NsOperand A{slice + c.a + (int64_t)ti * T * c.lp, splane, c.lp, c.p - ti * T}, B{slice + c.b + tj * T, yplane, c.lq, qq - tj * T};
   f32x16 acc[TL::FM][TL::FN];
   ns_product<TL, PARTS, true, !TALL>(acc, A, B, pp, lds);
   const MuonMat a = t.mats[c.mat0 + z];
@@ -629,23 +636,24 @@ hipError_t launch_muon_begin(const MuonEntry* entries, const MuonMat* mats, int 
 
 namespace {
 
-// the classes that `take` accepts, with the workgroups that `tiles` gives per matrix
+// the jobs that `take` accepts, with the workgroups that `tiles` gives per matrix
 template <class Take, class Tiles>
 NsArgs laid_out(const NsArgs& a, Take&& take, Tiles&& tiles) {
-  NsArgs o = {};
-  for (int k = 0; k < a.nclass; ++k) {
-    if (!take(a.c[k])) continue;
-    o.c[o.nclass] = a.c[k];
-    o.c[o.nclass++].first = o.total;
-    o.total += a.c[k].nb * tiles(a.c[k]);
+  NsArgs o;
+  o.count = o.total = 0;
+  for (int k = 0; k < a.count; ++k) {
+    if (!take(a.j[k])) continue;
+    o.j[o.count] = a.j[k];
+    o.j[o.count++].first = o.total;
+    o.total += a.j[k].nb * tiles(a.j[k]);
   }
   return o;
 }
 
 int ceil_div(int a, int b) { return (a + b - 1) / b; }
-bool any(const NsClass&) { return true; }
+bool any(const NsJob&) { return true; }
 
-// more than 64 KB of LDS have to be asked for, once per kernel and device
+// more than 64 KB of LDS have to be asked for
 template <class K>
 hipError_t allow_lds(K* kernel, int bytes) {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -654,63 +662,66 @@ hipError_t allow_lds(K* kernel, int bytes) {
 template <class TL, class K, class... A>
 hipError_t go(K* kernel, const NsArgs& a, hipStream_t st, A... rest) {
   if (a.total == 0) return hipSuccess;
-  if (TL::LDS > 65536) {
-    const hipError_t rc = allow_lds(kernel, TL::LDS);
-    if (rc != hipSuccess) return rc;
-  }
+  const hipError_t rc = allow_lds(kernel, TL::LDS);
+  if (rc != hipSuccess) return rc;
   kernel<<<a.total, TL::THREADS, TL::LDS, st>>>(a, rest...);
   return hipGetLastError();
 }
 
 typedef NsTile<128, 2, 2> Small;
+typedef NsTile<256, 2, 4> Large;
 
-template <class TL>
-NsArgs upper(const NsArgs& a) {
-  return laid_out(a, any, [](const NsClass& c) { const int n = ceil_div(c.p, TL::T); return n * (n + 1) / 2; });
+template <int T>
+int tiles_of(const NsJob& c) {
+  const int n = ceil_div(c.p, T);
+  return c.kind == NS_APPLY ? n * ceil_div(c.q, T) : n * (n + 1) / 2;
 }
-template <class TL>
-int full(const NsClass& c) { return ceil_div(c.p, TL::T) * ceil_div(c.q, TL::T); }
+
+#ifndef WIDE
+#define WIDE 160
+#endif
+bool large(const NsArgs& a) {
+  int64_t n = 0;
+  for (int k = 0; k < a.count; ++k) n += (int64_t)a.j[k].nb * tiles_of<256>(a.j[k]);
+  return n >= WIDE;
+}
 
 template <class TL, int PARTS, bool XBF>
-hipError_t final_of(const NsArgs& a, const MuonTables& t, int src, float s, bool update, float keep, float lr, hipStream_t st) {
-  const hipError_t rc = go<TL>(k_ns_final<TL, PARTS, XBF, false>, laid_out(a, [](const NsClass& c) { return !c.tall; }, full<TL>), st, t, src, s, (int)update, keep, lr);
+hipError_t final_of(const NsArgs& a, const MuonTables& t, bool update, float keep, float lr, hipStream_t st) {
+  const hipError_t rc = go<TL>(k_ns_final<TL, PARTS, XBF, false>, laid_out(a, [](const NsJob& c) { return !c.tall; }, tiles_of<TL::T>), st, t, (int)update, keep, lr);
   if (rc != hipSuccess) return rc;
-  return go<TL>(k_ns_final<TL, PARTS, XBF, true>, laid_out(a, [](const NsClass& c) { return c.tall != 0; }, full<TL>), st, t, src, s, (int)update, keep, lr);
+  return go<TL>(k_ns_final<TL, PARTS, XBF, true>, laid_out(a, [](const NsJob& c) { return c.tall != 0; }, tiles_of<TL::T>), st, t, (int)update, keep, lr);
+}
+
+template <class TL>
+hipError_t products_of(const NsArgs& a, int parts, hipStream_t st) {
+  const NsArgs o = laid_out(a, any, tiles_of<TL::T>);
+  return parts == 2 ? go<TL>(k_ns_products<TL, 2>, o, st) : go<TL>(k_ns_products<TL, 1>, o, st);
+}
+
+template <class TL>
+hipError_t final_tiles(const NsArgs& a, const MuonTables& t, int parts, bool update, float keep, float lr, bool x_bf16, hipStream_t st) {
+  if (parts == 2) return x_bf16 ? final_of<TL, 2, true>(a, t, update, keep, lr, st) : final_of<TL, 2, false>(a, t, update, keep, lr, st);
+  return x_bf16 ? final_of<TL, 1, true>(a, t, update, keep, lr, st) : final_of<TL, 1, false>(a, t, update, keep, lr, st);
 }
 
 }  // namespace
 
 hipError_t launch_muon_scale(const NsArgs& a, const MuonTables& t, float mu, bool nesterov, bool g_bf16, int parts, double eps,
                              double scale, hipStream_t st) {
-  const NsArgs o = laid_out(a, any, [](const NsClass& c) { return ceil_div(c.p, 64) * ceil_div(c.q, 64); });
+  const NsArgs o = laid_out(a, any, [](const NsJob& c) { return ceil_div(c.p, 64) * ceil_div(c.q, 64); });
   auto run = [&](auto kernel) { kernel<<<o.total, 256, 0, st>>>(o, t, mu, (int)nesterov, eps, scale); };
   if (g_bf16) parts == 2 ? run(k_muon_scale<true, 2>) : run(k_muon_scale<true, 1>);
   else parts == 2 ? run(k_muon_scale<false, 2>) : run(k_muon_scale<false, 1>);
   return hipGetLastError();
 }
 
-hipError_t launch_ns_gram(const NsArgs& a, int parts, int src, float out_scale, hipStream_t st) {
-  const NsPoly k{0.f, 0.f, out_scale};
-  const NsArgs o = upper<Small>(a);
-  return parts == 2 ? go<Small>(k_ns_sym<Small, 2, false>, o, st, src, k) : go<Small>(k_ns_sym<Small, 1, false>, o, st, src, k);
+hipError_t launch_ns_products(const NsArgs& a, int parts, hipStream_t st) {
+  return large(a) ? products_of<Large>(a, parts, st) : products_of<Small>(a, parts, st);
 }
 
-hipError_t launch_ns_poly(const NsArgs& a, int parts, float ca, float cb, float cc, float s_scale, float out_scale, hipStream_t st) {
-  const NsPoly k{ca * out_scale, cb * out_scale / s_scale, cc * out_scale / (s_scale * s_scale)};
-  const NsArgs o = upper<Small>(a);
-  return parts == 2 ? go<Small>(k_ns_sym<Small, 2, true>, o, st, 0, k) : go<Small>(k_ns_sym<Small, 1, true>, o, st, 0, k);
-}
-
-hipError_t launch_ns_apply(const NsArgs& a, int parts, int src, float out_scale, hipStream_t st) {
-  const NsArgs o = laid_out(a, any, full<Small>);
-  return parts == 2 ? go<Small>(k_ns_apply<Small, 2>, o, st, src, out_scale) : go<Small>(k_ns_apply<Small, 1>, o, st, src, out_scale);
-}
-
-hipError_t launch_ns_final(const NsArgs& a, const MuonTables& t, int parts, int src, float out_scale, bool update, float keep, float lr,
-                           bool x_bf16, hipStream_t st) {
-  if (parts == 2)
-    return x_bf16 ? final_of<Small, 2, true>(a, t, src, out_scale, update, keep, lr, st) : final_of<Small, 2, false>(a, t, src, out_scale, update, keep, lr, st);
-  return x_bf16 ? final_of<Small, 1, true>(a, t, src, out_scale, update, keep, lr, st) : final_of<Small, 1, false>(a, t, src, out_scale, update, keep, lr, st);
+hipError_t launch_ns_final(const NsArgs& a, const MuonTables& t, int parts, bool update, float keep, float lr, bool x_bf16, hipStream_t st) {
+  return large(a) ? final_tiles<Large>(a, t, parts, update, keep, lr, x_bf16, st) : final_tiles<Small>(a, t, parts, update, keep, lr, x_bf16, st);
 }
 
 }  // namespace od

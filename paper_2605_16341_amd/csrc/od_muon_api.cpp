@@ -15,7 +15,7 @@ using od::MuonEntry;
 using od::MuonMat;
 using od::MuonTables;
 using od::NsArgs;
-using od::NsClass;
+using od::NsJob;
 
 constexpr size_t kAlign = 256;
 constexpr int64_t kMaxDim = 1 << 22;       // 32-bit offsets of the operand loads: 256 rows of 2^22 fp16 words
@@ -29,16 +29,46 @@ int up64(int64_t v) { return (int)((v + 63) / 64 * 64); }
 // rows a multiple of 2 KB apart would put the rows of a tile on few memory channels
 int pitch(int64_t v) { return up64(v) % 1024 == 0 ? up64(v) + 64 : up64(v); }
 
+constexpr int kMostSymmetric = 5;          // symmetric matrices of a slice
+
+// Operands of a job: Y buffer 0 or 1, or symmetric matrix 0 ..; Y comes first in a slice.
+struct Operand { bool y; int index; };
+struct PlannedJob {
+  od::NsKind kind;
+  Operand a, b, e, out;
+  float ca, cb, cc;
+};
+// What a class does from its scaled input on: stage s of every class is one launch, the last job the final product.
+struct Plan {
+  std::vector<std::vector<PlannedJob>> stages;
+  PlannedJob last;
+  int symmetric;                           // matrices that the jobs use
+};
+
+struct Class {
+  NsJob job;                               // shape, slices and tables; base from the call
+  size_t offset;                           // bytes of its slices behind the cluster's start
+  const Plan* plan;
+};
 struct Cluster {
-  NsArgs args;                             // `first` is left to the launchers, base to the call
-  std::vector<int64_t> offset;             // bytes of the classes' slices behind the cluster's start
+  std::vector<Class> classes;
   int mat0, count;                         // rows of the matrix tables
 };
 
-struct Iteration {
-  float a, b, c;
-  int exp_y, exp_s, exp_p, exp_out;        // powers of two of the stored words: Y read, S, P, Y written
-};
+// Steps of one segment share their S = Y Y^T (see od_muon.hip).  Every S = P S P multiplies the rounding errors of S in
+// the directions of small singular values by up to max |P|^2, as it multiplies those singular values themselves; what counts is
+// how far that has gone where P stops being flat, a later segment starts there.  With these limits on the product of
+// max |P|^2 over a segment the published coefficients are cut 3 + 2.  Emulated in fp16 on 256 x 1024 to 1024 x 4096 matrices (power-law,
+// spiked and flat spectra), relative error of O: 0.9 to 2.7e-3 step by step, 1.0 to 3.5e-3 cut 3 + 2, 2.3 to 11e-3 cut 2 + 3, 1.3e-3
+// to 0.47 in one segment; with two fp16 words 1.6 to 6.1e-6, 2.5 to 5.1e-6, 2.7 to 13e-6 and 2 to 400e-6.
+constexpr double kFirstGrowth = 150.0, kLaterGrowth = 12.5;
+// In units of p^3 a step by itself costs 3 rho + 1 with rho = q / p, a segment of L steps 3 rho + 4 L - 3: the same for two
+// segments of 3 + 2 and five steps at rho = 1.  But a segment has more and smaller launches.
+#ifndef SEG_P
+#define SEG_P 512
+#endif
+constexpr int kSegmentRows = SEG_P;
+bool takes_segments(int p, int q) { return p >= kSegmentRows && 4 * (int64_t)q >= 5 * (int64_t)p; }
 
 // power of two that brings values up to `bound` to 2^13 at most, three bits below the end of fp16's range
 int exponent_for(double bound) { return 13 - (int)std::ceil(std::log2(bound)); }
@@ -49,7 +79,8 @@ struct orthdion_muon_ctx {
   std::vector<orthdion_muon_matdesc> mats;
   orthdion_muon_config cfg;
   int parts;
-  std::vector<Iteration> iterations;
+  Plan step_by_step, segments;
+  int first_exp;                           // power of two of the scaled input
   std::vector<int> order;                  // table row -> matrix
   std::vector<MuonMat> table;              // by row
   std::vector<Cluster> clusters;
@@ -68,31 +99,116 @@ static int no_throw(F&& body) {
   }
 }
 
-// Powers of two from bounds on the spectral norms, which bound every entry: sigma <= 1 at the start (Frobenius norm 1),
-// then the largest |sigma (a + b sigma^2 + c sigma^4)| over the range before, with 2 % for the rounding of the iterate.
-static int plan_iterations(orthdion_muon_ctx* h) {
+struct Step {
+  double a, b, c;
+  double top;                              // bound of the singular values it starts from
+  double poly;                             // of |a + b s^2 + c s^4| over them
+};
+
+// Powers of two of the stored words follow from bounds on the spectral norms, which bound every entry: sigma <= 1 at the start
+// (Frobenius norm 1), then the largest |sigma (a + b sigma^2 + c sigma^4)| over the range before, with 2 % for rounding.
+static int plan_steps(const orthdion_muon_config& cfg, std::vector<Step>* steps) {
   double top = 1.02;
-  for (int k = 0; k < h->cfg.steps; ++k) {
-    Iteration it;
-    it.a = h->cfg.coeffs[3 * k]; it.b = h->cfg.coeffs[3 * k + 1]; it.c = h->cfg.coeffs[3 * k + 2];
-    if (!std::isfinite(it.a) || !std::isfinite(it.b) || !std::isfinite(it.c)) return ORTHDION_E_INVALID_ARG;
-    double poly = 0.0, next = 0.0;
+  for (int k = 0; k < cfg.steps; ++k) {
+    Step s{cfg.coeffs[3 * k], cfg.coeffs[3 * k + 1], cfg.coeffs[3 * k + 2], top, 0.0};
+    if (!std::isfinite(s.a) || !std::isfinite(s.b) || !std::isfinite(s.c)) return ORTHDION_E_INVALID_ARG;
+    double next = 0.0;
     for (int i = 0; i <= 4096; ++i) {
-      const double s = top * i / 4096, v = std::fabs(it.a + it.b * s * s + it.c * s * s * s * s);
-      poly = std::max(poly, v);
-      next = std::max(next, v * s);
+      const double x = top * i / 4096, v = std::fabs(s.a + s.b * x * x + s.c * x * x * x * x);
+      s.poly = std::max(s.poly, v);
+      next = std::max(next, v * x);
     }
-    if (!(poly <= 256.0) || !(next <= 32.0)) return ORTHDION_E_INVALID_ARG;
-    poly = std::max(1.02 * poly, 1.0 / 256);
-    next = std::max(1.02 * next, 1.0 / 256);
-    it.exp_y = exponent_for(top);
-    it.exp_s = exponent_for(top * top);
-    it.exp_p = exponent_for(poly);
-    it.exp_out = exponent_for(next);
-    h->iterations.push_back(it);
-    top = next;
+    if (!(s.poly <= 256.0) || !(next <= 32.0)) return ORTHDION_E_INVALID_ARG;
+    s.poly = std::max(1.02 * s.poly, 1.0 / 256);
+    top = std::max(1.02 * next, 1.0 / 256);
+    steps->push_back(s);
   }
+  steps->push_back(Step{0.0, 0.0, 0.0, top, 1.0});            // the bound behind the last step
   return ORTHDION_OK;
+}
+
+// bound of |P_0 P_1 .. P_(count - 1)| of the steps from `from` on
+static double product_bound(const std::vector<Step>& steps, int from, int count) {
+  double most = 0.0;
+  for (int i = 0; i <= 4096; ++i) {
+    double x = steps[from].top * i / 4096, z = 1.0;
+    for (int k = from; k < from + count; ++k) {
+      const double v = steps[k].a + steps[k].b * x * x + steps[k].c * x * x * x * x;
+      z *= v;
+      x *= std::fabs(v);
+    }
+    most = std::max(most, std::fabs(z));
+  }
+  return std::max(1.02 * most, 1.0 / 256);
+}
+
+static void plan_jobs(const std::vector<Step>& steps, bool segmented, Plan* plan) {
+  const int count = (int)steps.size() - 1;
+  const Operand none{false, 0}, s_mat{false, 0}, t_mat{false, 1};
+  auto two = [](int e) { return (float)std::ldexp(1.0, e); };
+  int src = 0;
+  plan->symmetric = 2;
+  for (int k = 0; k < count;) {
+    int length = 1;
+    if (segmented) {
+      double growth = 1.0;
+      while (k + length < count) {
+        growth *= steps[k + length - 1].poly * steps[k + length - 1].poly;
+        if (growth > (k == 0 ? kFirstGrowth : kLaterGrowth)) break;
+        ++length;
+      }
+    }
+    const int exp_y = exponent_for(steps[k].top);
+    // P and Z change between the matrices behind S and T (step by step: P alone, where T would be)
+    int free_mats[3] = {2, 3, 4};
+    Operand p_mat = length > 1 ? Operand{false, free_mats[0]} : t_mat, z_mat = p_mat;
+    if (length > 1) plan->symmetric = kMostSymmetric;
+    int exp_s = exponent_for(steps[k].top * steps[k].top), exp_p = exponent_for(steps[k].poly), exp_z = exp_p;
+    plan->stages.push_back({PlannedJob{od::NS_GRAM, {true, src}, {true, src}, none, s_mat, 0.f, 0.f, two(exp_s - 2 * exp_y)}});
+    auto poly = [&](const Step& st, Operand out) {
+      return PlannedJob{od::NS_SYM, s_mat, s_mat, s_mat, out, (float)(st.a * two(exp_p)), (float)(st.b * two(exp_p - exp_s)), (float)(st.c * two(exp_p - 2 * exp_s))};
+    };
+    plan->stages.push_back({poly(steps[k], p_mat)});
+    for (int l = 1; l < length; ++l) {
+      const Step& before = steps[k + l - 1];
+      const Step& st = steps[k + l];
+      // T = P S; and Z = P Z of the step before, unless it is P itself
+      const int exp_t = exponent_for(before.poly * before.top * before.top);
+      std::vector<PlannedJob> pair{PlannedJob{od::NS_SYM, p_mat, s_mat, none, t_mat, 0.f, 0.f, two(exp_t - exp_p - exp_s)}};
+      Operand new_z = z_mat;
+      if (l > 1) {
+        const int exp_new = exponent_for(product_bound(steps, k, l));
+        new_z = Operand{false, 2 + 3 + 4 - p_mat.index - z_mat.index};
+        pair.push_back(PlannedJob{od::NS_SYM, p_mat, z_mat, none, new_z, 0.f, 0.f, two(exp_new - exp_p - exp_z)});
+        exp_z = exp_new;
+      }
+      plan->stages.push_back(pair);
+      // S = T P
+      const int exp_new_s = exponent_for(st.top * st.top);
+      plan->stages.push_back({PlannedJob{od::NS_SYM, t_mat, p_mat, none, s_mat, 0.f, 0.f, two(exp_new_s - exp_t - exp_p)}});
+      exp_s = exp_new_s;
+      // the next P where neither Z nor, for its last use, the old P lies
+      z_mat = new_z;
+      exp_p = exponent_for(st.poly);
+      int index = 2;
+      while (index == z_mat.index) ++index;
+      p_mat = Operand{false, index};
+      plan->stages.push_back({poly(st, p_mat)});
+    }
+    if (length > 1) {
+      const int exp_new = exponent_for(product_bound(steps, k, length));
+      const Operand new_z{false, 2 + 3 + 4 - p_mat.index - z_mat.index};
+      plan->stages.push_back({PlannedJob{od::NS_SYM, p_mat, z_mat, none, new_z, 0.f, 0.f, two(exp_new - exp_p - exp_z)}});
+      z_mat = new_z;
+      exp_z = exp_new;
+    }
+    k += length;
+    const int exp_out = k < count ? exponent_for(steps[k].top) : 0;
+    const PlannedJob apply{od::NS_APPLY, z_mat, {true, src}, none, {true, 1 - src}, 0.f, 0.f, two(exp_out - exp_z - exp_y)};
+    if (k < count) plan->stages.push_back({apply});
+    else plan->last = apply;
+    src = 1 - src;
+  }
 }
 
 static int check_muon_config(const orthdion_muon_config* c) {
@@ -124,30 +240,35 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
   *out = h;                                // the caller frees it if anything below fails or throws
   h->mats.assign(mats, mats + nmat);
   h->cfg = *cfg;
-  if ((rc = plan_iterations(h)) != ORTHDION_OK) return rc;
+  std::vector<Step> steps;
+  if ((rc = plan_steps(*cfg, &steps)) != ORTHDION_OK) return rc;
+  plan_jobs(steps, false, &h->step_by_step);
+  plan_jobs(steps, true, &h->segments);
+  h->first_exp = exponent_for(steps[0].top);
   const bool exact = cfg->precision == ORTHDION_PREC_EXACT ||
                      (cfg->precision == ORTHDION_PREC_AUTO && !(cfg->x_dtype == ORTHDION_BF16 && cfg->g_dtype == ORTHDION_BF16));
   h->parts = exact ? 2 : 1;
 
   // classes in order of first appearance
-  struct Class { int p, q, tall; std::vector<int> members; };
-  std::vector<Class> classes;
+  struct Shape { int p, q, tall; std::vector<int> members; };
+  std::vector<Shape> classes;
   for (int i = 0; i < nmat; ++i) {
     const int p = (int)std::min(mats[i].m, mats[i].n), q = (int)std::max(mats[i].m, mats[i].n), tall = mats[i].m > mats[i].n;
     size_t k = 0;
     while (k < classes.size() && !(classes[k].p == p && classes[k].q == q && classes[k].tall == tall)) ++k;
-    if (k == classes.size()) classes.push_back(Class{p, q, tall, {}});
+    if (k == classes.size()) classes.push_back(Shape{p, q, tall, {}});
     classes[k].members.push_back(i);
   }
   // clusters
   int64_t held = 0;
   size_t slices = 0, most = 0;
-  for (const Class& c : classes) {
+  for (const Shape& c : classes) {
     const int64_t elements = (int64_t)c.p * c.q;
     const int lp = pitch(c.p), lq = pitch(c.q);
-    const int64_t stride = h->parts * 2 * (od::ns_y_plane(c.p, lq) + od::ns_s_plane(c.p, lp));
+    const Plan& plan = takes_segments(c.p, c.q) ? h->segments : h->step_by_step;
+    const int64_t stride = h->parts * (2 * od::ns_y_plane(c.p, lq) + plan.symmetric * od::ns_s_plane(c.p, lp));
     for (size_t done = 0; done < c.members.size();) {
-      if (h->clusters.empty() || held + elements > kClusterElements || h->clusters.back().args.nclass == od::kNsClasses) {
+      if (h->clusters.empty() || held + elements > kClusterElements || (int)h->clusters.back().classes.size() == od::kNsClasses) {
         h->clusters.push_back(Cluster{});
         h->clusters.back().mat0 = (int)h->order.size();
         held = 0;
@@ -157,9 +278,11 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
       const int64_t room = std::max((int64_t)1, (kClusterElements - held) / elements);
       // the workgroups of a launch are counted in 32 bits: a class of many matrices is 64 x 64 tiles at least
       const int take = (int)std::min<int64_t>({room, (int64_t)(c.members.size() - done), 1 << 20});
-      NsClass& n = cl.args.c[cl.args.nclass++];
-      n = NsClass{0, c.p, c.q, lp, lq, take, (int)h->order.size(), c.tall, nullptr, stride};
-      cl.offset.push_back((int64_t)slices);
+      NsJob job = {};
+      job.p = c.p; job.q = c.q; job.lp = lp; job.lq = lq; job.nb = take; job.tall = c.tall;
+      job.mat0 = (int)h->order.size();
+      job.stride = stride;
+      cl.classes.push_back(Class{job, slices, &plan});
       slices = align_up(slices + (size_t)take * (size_t)stride * 2);
       most = std::max(most, slices);
       for (int k = 0; k < take; ++k) {
@@ -217,23 +340,38 @@ static int muon_run(orthdion_muon_handle h, void* const* X, const void* const* G
                      reinterpret_cast<double*>(ws + h->off_partials), reinterpret_cast<int*>(ws + h->off_info)};
   const bool gbf = h->cfg.g_dtype == ORTHDION_BF16, xbf = h->cfg.x_dtype == ORTHDION_BF16, nesterov = h->cfg.nesterov != 0;
   const float keep = (float)(1.0 - (double)h->cfg.lr * (double)h->cfg.weight_decay);
+  const int parts = h->parts;
   for (const Cluster& cl : h->clusters) {
-    NsArgs a = cl.args;
-    for (int k = 0; k < a.nclass; ++k) a.c[k].base = reinterpret_cast<uint16_t*>(ws + h->off_slices + cl.offset[k]);
+    NsArgs args;
+    auto add = [&](const Class& c, const PlannedJob& job) {
+      NsJob& j = args.j[args.count++];
+      j = c.job;
+      j.base = reinterpret_cast<uint16_t*>(ws + h->off_slices + c.offset);
+      auto at = [&](const Operand& o) {
+        const int64_t y = od::ns_y_plane(j.p, j.lq) * parts;
+        return o.y ? o.index * y : 2 * y + o.index * od::ns_s_plane(j.p, j.lp) * parts;
+      };
+      j.kind = job.kind;
+      j.a = at(job.a); j.b = at(job.b); j.e = at(job.e); j.out = at(job.out);
+      j.ca = job.ca; j.cb = job.cb; j.cc = job.cc;
+    };
     OD_TRY(od::launch_muon_begin(entries.get() + cl.mat0, h->table.data() + cl.mat0, cl.mat0, cl.count, t, h->cfg.mu, nesterov, gbf, st));
-    OD_TRY(od::launch_muon_scale(a, t, h->cfg.mu, nesterov, gbf, h->parts, h->cfg.eps, std::ldexp(1.0, h->iterations[0].exp_y), st));
-    const int steps = (int)h->iterations.size();
-    for (int k = 0; k < steps; ++k) {
-      const Iteration& it = h->iterations[k];
-      const int src = k & 1;
-      OD_TRY(od::launch_ns_gram(a, h->parts, src, std::ldexp(1.f, it.exp_s - 2 * it.exp_y), st));
-      OD_TRY(od::launch_ns_poly(a, h->parts, it.a, it.b, it.c, std::ldexp(1.f, it.exp_s), std::ldexp(1.f, it.exp_p), st));
-      if (k + 1 < steps) {
-        OD_TRY(od::launch_ns_apply(a, h->parts, src, std::ldexp(1.f, it.exp_out - it.exp_p - it.exp_y), st));
-      } else {
-        OD_TRY(od::launch_ns_final(a, t, h->parts, src, std::ldexp(1.f, -it.exp_p - it.exp_y), update, keep, h->cfg.lr, xbf, st));
-      }
+    args.count = 0;
+    size_t stages = 0;
+    for (const Class& c : cl.classes) {
+      add(c, c.plan->last);
+      stages = std::max(stages, c.plan->stages.size());
     }
+    OD_TRY(od::launch_muon_scale(args, t, h->cfg.mu, nesterov, gbf, parts, h->cfg.eps, std::ldexp(1.0, h->first_exp), st));
+    const NsArgs last = args;
+    for (size_t s = 0; s < stages; ++s) {
+      args.count = 0;
+      for (const Class& c : cl.classes)
+        if (s < c.plan->stages.size())
+          for (const PlannedJob& job : c.plan->stages[s]) add(c, job);
+      OD_TRY(od::launch_ns_products(args, parts, st));
+    }
+    OD_TRY(od::launch_ns_final(last, t, parts, update, keep, h->cfg.lr, xbf, st));
   }
   return ORTHDION_OK;
 }
