@@ -38,7 +38,10 @@ struct MuonMat {                           // one matrix, as the elementwise ker
 enum NsKind : int {
   NS_GRAM = 0,                             // out = cc a a^T of Y at a
   NS_SYM = 1,                              // out = ca I + cb e + cc a b of commuting symmetric a, b; e read where cb != 0
-  NS_APPLY = 2                             // out = cc a b of symmetric a and Y at b
+  NS_APPLY = 2,                            // out = cc a b of p x p a and Y at b
+  NS_FULL = 3,                             // out = cc a b of symmetric a, b, not mirrored
+  NS_REDUCE = 4,                           // out = cc (sum of the partial sums at a)
+  NS_SMALL = 5                             // out = Z of a segment of steps from cc (sum of the partial sums at a)
 };
 struct NsJob {
   int first;                               // first workgroup of the job
@@ -50,16 +53,37 @@ struct NsJob {
   int64_t a, b, e, out;                    // operands in a slice, elements
   float ca, cb, cc;
   int kind;
+  int splits;                              // NS_GRAM: > 0: that many partial sums of the K range, fp32 at out, for another
+                                           // kernel to add up
 };
 
-struct NsArgs {
+template <int N>
+struct NsJobs {
   int count, total;                        // jobs, workgroups
-  NsJob j[kNsJobs];
+  NsJob j[N];
 };
+typedef NsJobs<kNsJobs> NsArgs;            // with the tables' pointers below the 4 KB of a launch's arguments
 
 // elements of a slice
 inline int64_t ns_y_plane(int p, int lq) { return (int64_t)((p + kNsStep - 1) / kNsStep * kNsStep) * lq; }
 inline int64_t ns_s_plane(int p, int lp) { return (int64_t)p * lp; }
+
+// Partial sums of a matrix: [tile of the upper triangle][split][kNsSplitTile * kNsSplitTile], row by row, rounded up to whole
+// groups of kNsStep fp16 words.
+constexpr int kNsSplitTile = 128;
+inline int64_t ns_partials(int p, int splits) {
+  const int64_t n = (p + kNsSplitTile - 1) / kNsSplitTile;
+  return n * (n + 1) / 2 * splits * kNsSplitTile * kNsSplitTile * 2;
+}
+
+// Steps of a segment for the kernel that does all p x p work of a small matrix in LDS: coefficients and the powers of two
+// of the words of S, P, T = P S and Z that step k writes.
+constexpr int kNsSmall = 128;              // largest p
+constexpr int kNsMostSteps = 32;
+struct NsSteps {
+  int count;
+  float a[kNsMostSteps], b[kNsMostSteps], c[kNsMostSteps], s[kNsMostSteps], p[kNsMostSteps], t[kNsMostSteps], z[kNsMostSteps];
+};
 
 struct MuonTables {                        // in the workspace, one row per matrix
   MuonEntry* entries;
@@ -75,8 +99,11 @@ hipError_t launch_muon_begin(const MuonEntry* entries, const MuonMat* mats, int 
 // Y = B * (scale / (||B||_F + eps)) in fp16 words, zero padding, info words; one job per class
 hipError_t launch_muon_scale(const NsArgs& a, const MuonTables& t, float mu, bool nesterov, bool g_bf16, int parts, double eps,
                              double scale, hipStream_t st);
-// the products of the jobs
+// jobs of kinds up to NS_FULL; of NS_REDUCE; of NS_SMALL (one list of steps for all)
 hipError_t launch_ns_products(const NsArgs& a, int parts, hipStream_t st);
+hipError_t launch_ns_reduce(const NsArgs& a, int parts, hipStream_t st);
+// p up to kNsSmall
+hipError_t launch_ns_small(const NsArgs& a, const NsSteps& steps, int parts, hipStream_t st);
 // O = cc a b of jobs of kind NS_APPLY, into the callers' matrices: X = O, or with `update` X = keep X - lr scale_i O
 hipError_t launch_ns_final(const NsArgs& a, const MuonTables& t, int parts, bool update, float keep, float lr, bool x_bf16, hipStream_t st);
 

@@ -135,7 +135,8 @@ OD_DEV void split2(float a, float b, uint32_t* out) {
   }
 }
 
-OD_DEV int ns_job(const NsArgs& a, int bid) {
+template <int N>
+OD_DEV int ns_job(const NsJobs<N>& a, int bid) {
   int k = 0;
   while (k + 1 < a.count && bid >= a.j[k + 1].first) ++k;
   return k;
@@ -274,7 +275,7 @@ struct NsTile {
 
 // ACROSS: the accumulator of lane l holds C[l % 32][4 consecutive columns], otherwise C[4 consecutive rows][l % 32]
 template <class TL, int PARTS, bool TRB, bool ACROSS>
-OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const NsOperand& B, int kdim, char* lds) {
+OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const NsOperand& B, int kdim, char* lds, int split = 0, int splits = 1) {
   constexpr int T = TL::T, CH = TL::CH;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -294,13 +295,15 @@ OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const 
       vb[j] = (uint32_t)min(row, B.rows - 1) * (uint32_t)(B.ld * 2) + kg * 16;
     }
   }
-  const int ks = kdim / kNsStep, steps = ks * (PARTS == 2 ? 3 : 1);
+  const int ks = kdim / kNsStep, all = ks * (PARTS == 2 ? 3 : 1);
+  // steps first .. of all, this split's share
+  const int first = splits > 1 ? quotient(all * split, splits) : 0, steps = (splits > 1 ? quotient(all * (split + 1), splits) : all) - first;
   const int64_t bstep = TRB ? (int64_t)kNsStep * B.ld : kNsStep;
   // loads of one operand tile of one step; of a step past the last one, none
   struct Loads { const uint16_t* p; uint32_t at, mask; };
   auto slot = [&](int unit) { return (uint32_t)(unit % TL::RING) * TL::OPER; };
   auto loads_of = [&](int step, bool of_b) {
-    const int seg = PARTS == 2 ? quotient(step, ks) : 0, kk = PARTS == 2 ? step - seg * ks : step;
+    const int seg = PARTS == 2 ? quotient(first + step, ks) : 0, kk = first + step - seg * ks;
     const uint16_t* p = of_b ? B.p + (seg == 1 ? B.plane : 0) + kk * bstep : A.p + (seg == 2 ? A.plane : 0) + (int64_t)kk * kNsStep;
     return Loads{p, lds0 + slot(2 * step + of_b) + wave * CH * 1024, step < steps ? ~0u : 0u};
   };
@@ -512,16 +515,32 @@ __global__ __launch_bounds__(TL::THREADS, TL::BLOCKS) void k_ns_products(NsArgs 
       for (int e = 0; e < 4; ++e) x[e] = c.cc * acc[i][j][4 * v4 + e];
     }, slice + c.out, yplane, c.lq, row0, col0, c.p, qq, c.q, false);
   } else {
-    const int per = ni * (ni + 1) / 2;
-    const int z = quotient(local, per);
+    const bool full = c.kind == NS_FULL;
+    const int splits = c.splits > 0 ? c.splits : 1, tiles = full ? ni * ni : ni * (ni + 1) / 2, per = tiles * splits;
+    const int z = quotient(local, per), in_z = local - z * per, tile = quotient(in_z, splits), split = in_z - tile * splits;
     int ti, tj;
-    upper_tile(local - z * per, ni, &ti, &tj);
+    if (full) {
+      tj = quotient(tile, ni);
+      ti = tile - tj * ni;
+    } else {
+      upper_tile(tile, ni, &ti, &tj);
+    }
     uint16_t* slice = c.base + z * c.stride;
     const bool gram = c.kind == NS_GRAM;
     const int64_t plane = gram ? yplane : splane;
     const int ld = gram ? c.lq : c.lp;
     const NsOperand A{slice + c.a + (int64_t)ti * T * ld, plane, ld, c.p - ti * T}, B{slice + c.b + (int64_t)tj * T * ld, plane, ld, c.p - tj * T};
-    ns_product<TL, PARTS, false, true>(acc, A, B, gram ? qq : pp, lds);
+    ns_product<TL, PARTS, false, true>(acc, A, B, gram ? qq : pp, lds, split, splits);
+    if (c.splits > 0) {
+      const int lane = threadIdx.x & 63;
+      float* out = reinterpret_cast<float*>(slice + c.out) + (int64_t)in_z * T * T;
+      static_for<TL::FM * TL::FN * 4>([&](auto n) {
+        constexpr int i = decltype(n)::value / (4 * TL::FN), j = decltype(n)::value / 4 % TL::FN, v4 = decltype(n)::value % 4;
+        const int r = wave / TL::WJ * TL::WTM + 32 * i + (lane & 31), cl = wave % TL::WJ * TL::WTN + 32 * j + 8 * v4 + 4 * (lane >> 5);
+        *reinterpret_cast<f32x4*>(out + r * T + cl) = f32x4{acc[i][j][4 * v4], acc[i][j][4 * v4 + 1], acc[i][j][4 * v4 + 2], acc[i][j][4 * v4 + 3]};
+      });
+      return;
+    }
     __syncthreads();
     const int row0 = ti * T + wave / TL::WJ * TL::WTM, col0 = tj * T + wave % TL::WJ * TL::WTN;
     const uint16_t* E = slice + c.e;
@@ -543,7 +562,204 @@ __global__ __launch_bounds__(TL::THREADS, TL::BLOCKS) void k_ns_products(NsArgs 
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] = c.cc * acc[i][j][4 * v4 + e] + c.cb * s[e] + (row == col + e ? c.ca : 0.f);
-    }, slice + c.out, splane, c.lp, row0, col0, c.p, pp, c.p, ti != tj);
+    }, slice + c.out, splane, c.lp, row0, col0, c.p, pp, c.p, !full && ti != tj);
+  }
+}
+
+// Adds the partial sums of a Gram matrix in their order: one workgroup 32 rows of a tile, written in both triangles.
+template <int PARTS>
+__global__ __launch_bounds__(256) void k_ns_reduce(NsArgs args) {
+  constexpr int T = kNsSplitTile;
+  __shared__ float tile[32][T + 4];
+  const NsJob c = args.j[ns_job(args, blockIdx.x)];
+  const int pp = up64(c.p), n = (c.p + T - 1) / T, tiles = n * (n + 1) / 2, local = blockIdx.x - c.first;
+  const int z = quotient(local, 4 * tiles), in_z = local - z * 4 * tiles, t = in_z >> 2, part_rows = in_z & 3;
+  int ti, tj;
+  upper_tile(t, n, &ti, &tj);
+  uint16_t* slice = c.base + z * c.stride;
+  const float* in = reinterpret_cast<const float*>(slice + c.a) + (int64_t)t * c.splits * T * T + part_rows * 32 * T;
+  const int64_t splane = (int64_t)c.p * c.lp;
+  const int tid = threadIdx.x, r = tid >> 3, c0 = (tid & 7) * 4;
+  f32x4 sum[4] = {};
+  for (int s = 0; s < c.splits; ++s)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum[k] += *reinterpret_cast<const f32x4*>(in + (int64_t)s * T * T + r * T + c0 + 32 * k);
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) tile[r][c0 + 32 * k + e] = c.cc * sum[k][e];
+  __syncthreads();
+  uint16_t* out = slice + c.out;
+  // rows, eight columns a thread and turn
+  for (int k = tid; k < 32 * (T / 8); k += 256) {
+    const int row = ti * T + part_rows * 32 + k / (T / 8), col = tj * T + k % (T / 8) * 8;
+    if (row >= c.p || col >= pp) continue;
+    const float* v = &tile[k / (T / 8)][k % (T / 8) * 8];
+    u32x4 w[PARTS];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      uint32_t s[PARTS];
+      split2<PARTS>(col + 2 * e < c.p ? v[2 * e] : 0.f, col + 2 * e + 1 < c.p ? v[2 * e + 1] : 0.f, s);
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part) w[part][e] = s[part];
+    }
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) *reinterpret_cast<u32x4*>(out + part * splane + (int64_t)row * c.lp + col) = w[part];
+  }
+  if (ti == tj) return;
+  // columns as rows: the tile lies above the diagonal, so its rows are all inside
+  for (int k = tid; k < T * 4; k += 256) {
+    const int row = tj * T + k / 4, col = ti * T + part_rows * 32 + k % 4 * 8;
+    if (row >= c.p) continue;
+    u32x4 w[PARTS];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      uint32_t s[PARTS];
+      split2<PARTS>(tile[k % 4 * 8 + 2 * e][k / 4], tile[k % 4 * 8 + 2 * e + 1][k / 4], s);
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part) w[part][e] = s[part];
+    }
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) *reinterpret_cast<u32x4*>(out + part * splane + (int64_t)row * c.lp + col) = w[part];
+  }
+}
+
+// All p x p work of a segment of steps for one matrix of p <= D, in one workgroup: S and P lie in LDS as two fp16 words a
+// value (22 bits, three products), T = P S and Z in the accumulators' registers, from where they change places with S.
+// A chain of products with a barrier after each, about 1.5 us at D = 128; as launches of their own the same products take
+// 8 us each.
+template <int D>
+struct NsSmallTile {
+  static constexpr int WI = 2, WJ = D / 32, NW = WI * WJ, THREADS = 64 * NW, FM = D / 64;      // wave tile D/2 x 32
+  static constexpr int ROWB = D * 2, PLANE = D * ROWB, LDS = 4 * PLANE;
+};
+
+template <int D, int PARTS>
+__global__ __launch_bounds__(NsSmallTile<D>::THREADS, 1) void k_ns_small(NsJobs<kNsClasses> args, NsSteps k) {
+  typedef NsSmallTile<D> TL;
+  extern __shared__ __align__(16) char lds[];
+  const NsJob c = args.j[ns_job(args, blockIdx.x)];
+  const int z = blockIdx.x - c.first, pp = up64(c.p);
+  uint16_t* slice = c.base + z * c.stride;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row0 = wave / TL::WJ * (D / 2), col0 = wave % TL::WJ * 32;
+  typedef f32x16 Acc[TL::FM];
+  char* const s_plane = lds;
+  char* const p_plane = lds + 2 * TL::PLANE;
+  auto at = [](int row, int slot) { return row * TL::ROWB + ((slot ^ (D == 64 ? swz64(row) : row & 15)) << 4); };
+  // element e of entry v4 of accumulator i: row row0 + 32 i + lane % 32, column col0 + 8 v4 + 4 (lane / 32) + e
+  auto product = [&](const char* a, const char* b, Acc& out) {
+#pragma unroll
+    for (int i = 0; i < TL::FM; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) out[i][v] = 0.f;
+#pragma unroll 2
+    for (int ks = 0; ks < D / 16; ++ks) {
+      const int kg = 2 * ks + (lane >> 5);
+      u32x4 bh = *reinterpret_cast<const u32x4*>(b + at(col0 + (lane & 31), kg));
+      u32x4 bl = *reinterpret_cast<const u32x4*>(b + TL::PLANE + at(col0 + (lane & 31), kg));
+#pragma unroll
+      for (int i = 0; i < TL::FM; ++i) {
+        const u32x4 ah = *reinterpret_cast<const u32x4*>(a + at(row0 + 32 * i + (lane & 31), kg));
+        const u32x4 al = *reinterpret_cast<const u32x4*>(a + TL::PLANE + at(row0 + 32 * i + (lane & 31), kg));
+        out[i] = mfma_32x32x16<true>(bl, ah, out[i]);
+        out[i] = mfma_32x32x16<true>(bh, al, out[i]);
+        out[i] = mfma_32x32x16<true>(bh, ah, out[i]);
+      }
+    }
+  };
+  auto put = [&](char* plane, const Acc& v, float scale) {
+#pragma unroll
+    for (int i = 0; i < TL::FM; ++i)
+#pragma unroll
+      for (int v4 = 0; v4 < 4; ++v4) {
+        const int row = row0 + 32 * i + (lane & 31), col = col0 + 8 * v4 + 4 * (lane >> 5);
+        uint32_t a[2], b[2];
+        split2<2>(scale * v[i][4 * v4], scale * v[i][4 * v4 + 1], a);
+        split2<2>(scale * v[i][4 * v4 + 2], scale * v[i][4 * v4 + 3], b);
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+          *reinterpret_cast<u32x2*>(plane + part * TL::PLANE + at(row, col >> 3) + (col & 7) * 2) = u32x2{a[part], b[part]};
+      }
+  };
+  auto scaled = [](Acc& v, float f) {
+#pragma unroll
+    for (int i = 0; i < TL::FM; ++i)
+#pragma unroll
+      for (int n = 0; n < 16; ++n) v[i][n] *= f;
+  };
+  // S, zero outside the matrix
+  Acc s, p, zz, t;
+  {
+    const float* in = reinterpret_cast<const float*>(slice + c.a);
+#pragma unroll
+    for (int i = 0; i < TL::FM; ++i)
+#pragma unroll
+      for (int n = 0; n < 16; ++n) s[i][n] = 0.f;
+    for (int split = 0; split < c.splits; ++split)
+#pragma unroll
+      for (int i = 0; i < TL::FM; ++i)
+#pragma unroll
+        for (int v4 = 0; v4 < 4; ++v4) {
+          const int row = row0 + 32 * i + (lane & 31), col = col0 + 8 * v4 + 4 * (lane >> 5);
+          const f32x4 x = *reinterpret_cast<const f32x4*>(in + (int64_t)split * kNsSplitTile * kNsSplitTile + row * kNsSplitTile + col);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[i][4 * v4 + e] += row < c.p && col + e < c.p ? x[e] : 0.f;
+        }
+    scaled(s, c.cc);
+  }
+  for (int l = 0; l < k.count; ++l) {
+    if (l > 0) {
+      product(p_plane, s_plane, t);                       // T = P S
+      scaled(t, 1.f / (k.p[l - 1] * k.s[l - 1]));
+      __syncthreads();
+      if (l > 1) {
+        put(s_plane, zz, k.z[l - 2]);
+        __syncthreads();
+        product(p_plane, s_plane, zz);                    // Z = P Z
+        scaled(zz, 1.f / (k.p[l - 1] * k.z[l - 2]));
+        __syncthreads();
+      } else {
+#pragma unroll
+        for (int i = 0; i < TL::FM; ++i) zz[i] = p[i];
+      }
+      put(s_plane, t, k.t[l - 1]);
+      __syncthreads();
+      product(s_plane, p_plane, s);                       // S = T P
+      scaled(s, 1.f / (k.t[l - 1] * k.p[l - 1]));
+      __syncthreads();
+    }
+    put(s_plane, s, k.s[l]);
+    __syncthreads();
+    product(s_plane, s_plane, p);                         // P = a I + b S + c S S
+    const float ss = k.c[l] / (k.s[l] * k.s[l]);
+#pragma unroll
+    for (int i = 0; i < TL::FM; ++i)
+#pragma unroll
+      for (int n = 0; n < 16; ++n) {
+        const int row = row0 + 32 * i + (lane & 31), col = col0 + 8 * (n >> 2) + 4 * (lane >> 5) + (n & 3);
+        p[i][n] = k.b[l] * s[i][n] + ss * p[i][n] + (row == col && row < c.p ? k.a[l] : 0.f);
+      }
+    put(p_plane, p, k.p[l]);
+    __syncthreads();
+  }
+  if (k.count > 1) {
+    put(s_plane, zz, k.z[k.count - 2]);
+    __syncthreads();
+    product(p_plane, s_plane, p);                         // Z = P Z
+    scaled(p, 1.f / (k.p[k.count - 1] * k.z[k.count - 2]));
+  }
+  __syncthreads();
+  put(p_plane, p, k.z[k.count - 1]);
+  __syncthreads();
+  // Z out, rows of pp columns
+  const int64_t splane = (int64_t)c.p * c.lp;
+  for (int n = threadIdx.x; n < c.p * (pp / 8); n += TL::THREADS) {
+    const int row = n / (pp / 8), slot = n % (pp / 8);
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part)
+      *reinterpret_cast<u32x4*>(slice + c.out + part * splane + (int64_t)row * c.lp + 8 * slot) = *reinterpret_cast<const u32x4*>(p_plane + part * TL::PLANE + at(row, slot));
   }
 }
 
@@ -637,9 +853,9 @@ hipError_t launch_muon_begin(const MuonEntry* entries, const MuonMat* mats, int 
 namespace {
 
 // the jobs that `take` accepts, with the workgroups that `tiles` gives per matrix
-template <class Take, class Tiles>
-NsArgs laid_out(const NsArgs& a, Take&& take, Tiles&& tiles) {
-  NsArgs o;
+template <int N = kNsJobs, class Take, class Tiles>
+NsJobs<N> laid_out(const NsArgs& a, Take&& take, Tiles&& tiles) {
+  NsJobs<N> o;
   o.count = o.total = 0;
   for (int k = 0; k < a.count; ++k) {
     if (!take(a.j[k])) continue;
@@ -659,8 +875,8 @@ hipError_t allow_lds(K* kernel, int bytes) {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
-template <class TL, class K, class... A>
-hipError_t go(K* kernel, const NsArgs& a, hipStream_t st, A... rest) {
+template <class TL, class K, int N, class... A>
+hipError_t go(K* kernel, const NsJobs<N>& a, hipStream_t st, A... rest) {
   if (a.total == 0) return hipSuccess;
   const hipError_t rc = allow_lds(kernel, TL::LDS);
   if (rc != hipSuccess) return rc;
@@ -674,7 +890,7 @@ typedef NsTile<256, 2, 4> Large;
 template <int T>
 int tiles_of(const NsJob& c) {
   const int n = ceil_div(c.p, T);
-  return c.kind == NS_APPLY ? n * ceil_div(c.q, T) : n * (n + 1) / 2;
+  return c.kind == NS_APPLY ? n * ceil_div(c.q, T) : c.kind == NS_FULL ? n * n : n * (n + 1) / 2 * (c.splits > 0 ? c.splits : 1);
 }
 
 #ifndef WIDE
@@ -682,7 +898,10 @@ int tiles_of(const NsJob& c) {
 #endif
 bool large(const NsArgs& a) {
   int64_t n = 0;
-  for (int k = 0; k < a.count; ++k) n += (int64_t)a.j[k].nb * tiles_of<256>(a.j[k]);
+  for (int k = 0; k < a.count; ++k) {
+    if (a.j[k].splits > 0) return false;     // partial sums are those of tiles of kNsSplitTile
+    n += (int64_t)a.j[k].nb * tiles_of<256>(a.j[k]);
+  }
   return n >= WIDE;
 }
 
@@ -718,6 +937,29 @@ hipError_t launch_muon_scale(const NsArgs& a, const MuonTables& t, float mu, boo
 
 hipError_t launch_ns_products(const NsArgs& a, int parts, hipStream_t st) {
   return large(a) ? products_of<Large>(a, parts, st) : products_of<Small>(a, parts, st);
+}
+
+hipError_t launch_ns_reduce(const NsArgs& a, int parts, hipStream_t st) {
+  const NsArgs o = laid_out(a, any, [](const NsJob& c) { const int n = ceil_div(c.p, kNsSplitTile); return 4 * (n * (n + 1) / 2); });
+  if (parts == 2) k_ns_reduce<2><<<o.total, 256, 0, st>>>(o);
+  else k_ns_reduce<1><<<o.total, 256, 0, st>>>(o);
+  return hipGetLastError();
+}
+
+namespace {
+
+template <int D, int PARTS>
+hipError_t small_of(const NsArgs& a, const NsSteps& steps, hipStream_t st) {
+  const NsJobs<kNsClasses> o = laid_out<kNsClasses>(a, [](const NsJob& c) { return (c.p <= 64) == (D == 64); }, [](const NsJob&) { return 1; });
+  return go<NsSmallTile<D>>(k_ns_small<D, PARTS>, o, st, steps);
+}
+
+}  // namespace
+
+hipError_t launch_ns_small(const NsArgs& a, const NsSteps& steps, int parts, hipStream_t st) {
+  const hipError_t rc = parts == 2 ? small_of<64, 2>(a, steps, st) : small_of<64, 1>(a, steps, st);
+  if (rc != hipSuccess) return rc;
+  return parts == 2 ? small_of<128, 2>(a, steps, st) : small_of<128, 1>(a, steps, st);
 }
 
 hipError_t launch_ns_final(const NsArgs& a, const MuonTables& t, int parts, bool update, float keep, float lr, bool x_bf16, hipStream_t st) {

@@ -31,8 +31,9 @@ int pitch(int64_t v) { return up64(v) % 1024 == 0 ? up64(v) + 64 : up64(v); }
 
 constexpr int kMostSymmetric = 5;          // symmetric matrices of a slice
 
-// Operands of a job: Y buffer 0 or 1, or symmetric matrix 0 ..; Y comes first in a slice.
-struct Operand { bool y; int index; };
+// Operands of a job, in the order in which they lie in a slice: Y buffer 0 or 1, symmetric matrix 0 .., partial sums.
+enum Where { IN_Y, IN_SYMMETRIC, IN_PARTIALS };
+struct Operand { Where where; int index; };
 struct PlannedJob {
   od::NsKind kind;
   Operand a, b, e, out;
@@ -41,14 +42,19 @@ struct PlannedJob {
 // What a class does from its scaled input on: stage s of every class is one launch, the last job the final product.
 struct Plan {
   std::vector<std::vector<PlannedJob>> stages;
+  std::vector<od::NsSteps> steps;          // of the stages that are NS_SMALL, in order
   PlannedJob last;
   int symmetric;                           // matrices that the jobs use
 };
+// How: step by step, several steps on one Gram matrix, or those with all p x p work in one workgroup.
+enum Mode { STEP_BY_STEP, SEGMENTS, SMALL };
+constexpr int kModes = 3;
 
 struct Class {
   NsJob job;                               // shape, slices and tables; base from the call
   size_t offset;                           // bytes of its slices behind the cluster's start
   const Plan* plan;
+  int splits;                              // of its Gram matrices, 0: one sum
 };
 struct Cluster {
   std::vector<Class> classes;
@@ -57,18 +63,36 @@ struct Cluster {
 
 // Steps of one segment share their S = Y Y^T (see od_muon.hip).  Every S = P S P multiplies the rounding errors of S in
 // the directions of small singular values by up to max |P|^2, as it multiplies those singular values themselves; what counts is
-// how far that has gone where P stops being flat, a later segment starts there.  With these limits on the product of
-// max |P|^2 over a segment the published coefficients are cut 3 + 2.  Emulated in fp16 on 256 x 1024 to 1024 x 4096 matrices (power-law,
-// spiked and flat spectra), relative error of O: 0.9 to 2.7e-3 step by step, 1.0 to 3.5e-3 cut 3 + 2, 2.3 to 11e-3 cut 2 + 3, 1.3e-3
-// to 0.47 in one segment; with two fp16 words 1.6 to 6.1e-6, 2.5 to 5.1e-6, 2.7 to 13e-6 and 2 to 400e-6.
-constexpr double kFirstGrowth = 150.0, kLaterGrowth = 12.5;
+// how far that has gone where P stops being flat, a later segment starts there.  So a segment ends where the product of its
+// max |P|^2 would pass a limit.  Emulated on matrices of power-law, spiked and flat spectra, relative error of O for the published
+// coefficients:
+//   one fp16 word, 512 x 1024 to 1528 x 3304: step by step 0.9 to 3.0e-3, cut 2 + 2 + 1 1.2 to 2.4e-3, 3 + 2 0.9 to 2.7e-3,
+//   2 + 3 up to 9e-3, in one segment up to 0.5
+//   two words, 40 x 200 to 512 x 2048: step by step 1.1 to 6.1e-6, 2 + 1 + 2 1.1 to 5.2e-6, 2 + 2 + 1 1.2 to 5.2e-6 (twice as
+//   much as step by step on some), 3 + 2 1.1 to 7e-6
+//   one word for Y, two for the p x p work (small matrices), 40 x 200 to 300 x 700: 3 + 2 0.5 to 1.4e-3, in one segment 0.3 to 5.4e-3
+constexpr double kGrowth = 13.0, kSmallGrowth = 160.0;
 // In units of p^3 a step by itself costs 3 rho + 1 with rho = q / p, a segment of L steps 3 rho + 4 L - 3: the same for two
 // segments of 3 + 2 and five steps at rho = 1.  But a segment has more and smaller launches.
 #ifndef SEG_P
 #define SEG_P 512
 #endif
 constexpr int kSegmentRows = SEG_P;
-bool takes_segments(int p, int q) { return p >= kSegmentRows && 4 * (int64_t)q >= 5 * (int64_t)p; }
+Mode mode_for(int p, int q) {
+  if (p <= od::kNsSmall) return SMALL;
+  return p >= kSegmentRows && 4 * (int64_t)q >= 5 * (int64_t)p ? SEGMENTS : STEP_BY_STEP;
+}
+
+// Splits of the K range of a class's Gram matrices.  For the kernel that adds them up by itself (SMALL): its workgroup
+// reads 64 KB a split, about as long as two steps take, so the square root of the steps balances the two.  Otherwise
+// where the tiles leave most of the chip idle and the range is long: one round of workgroups, at least eight steps each.
+int splits_for(Mode mode, int p, int q, int nb, int parts) {
+  const int64_t steps = (int64_t)(up64(q) / od::kNsStep) * (parts == 2 ? 3 : 1);
+  if (mode == SMALL) return (int)std::min<int64_t>(16, std::max<int64_t>(1, (int64_t)std::lround(std::sqrt(0.6 * (double)steps))));
+  const int64_t n = (p + od::kNsSplitTile - 1) / od::kNsSplitTile, tiles = n * (n + 1) / 2 * nb;
+  if (tiles >= 128 || steps < 16) return 0;
+  return (int)std::min<int64_t>((256 + tiles - 1) / tiles, steps / 8);
+}
 
 // power of two that brings values up to `bound` to 2^13 at most, three bits below the end of fp16's range
 int exponent_for(double bound) { return 13 - (int)std::ceil(std::log2(bound)); }
@@ -79,7 +103,7 @@ struct orthdion_muon_ctx {
   std::vector<orthdion_muon_matdesc> mats;
   orthdion_muon_config cfg;
   int parts;
-  Plan step_by_step, segments;
+  Plan plans[2][kModes];                   // [Gram matrices in partial sums][mode]
   int first_exp;                           // power of two of the scaled input
   std::vector<int> order;                  // table row -> matrix
   std::vector<MuonMat> table;              // by row
@@ -142,29 +166,56 @@ static double product_bound(const std::vector<Step>& steps, int from, int count)
   return std::max(1.02 * most, 1.0 / 256);
 }
 
-static void plan_jobs(const std::vector<Step>& steps, bool segmented, Plan* plan) {
+static void plan_jobs(const std::vector<Step>& steps, Mode mode, bool split, int parts, Plan* plan) {
   const int count = (int)steps.size() - 1;
-  const Operand none{false, 0}, s_mat{false, 0}, t_mat{false, 1};
+  const Operand none{IN_SYMMETRIC, 0}, s_mat{IN_SYMMETRIC, 0}, t_mat{IN_SYMMETRIC, 1}, partials{IN_PARTIALS, 0};
   auto two = [](int e) { return (float)std::ldexp(1.0, e); };
   int src = 0;
-  plan->symmetric = 2;
+  plan->symmetric = mode == SMALL ? 1 : 2;
   for (int k = 0; k < count;) {
     int length = 1;
-    if (segmented) {
+    // two words: only the first and the last segment hold more than one step
+    if (mode != STEP_BY_STEP && (parts == 1 || k == 0 || k + 2 == count)) {
+      const double limit = k == 0 && mode == SMALL && parts == 1 ? kSmallGrowth : kGrowth;
       double growth = 1.0;
       while (k + length < count) {
         growth *= steps[k + length - 1].poly * steps[k + length - 1].poly;
-        if (growth > (k == 0 ? kFirstGrowth : kLaterGrowth)) break;
+        if (growth > limit) break;
         ++length;
       }
     }
     const int exp_y = exponent_for(steps[k].top);
+    auto apply_of = [&](const Operand& z, int exp_z) {
+      const int exp_out = k + length < count ? exponent_for(steps[k + length].top) : 0;
+      const PlannedJob apply{od::NS_APPLY, z, {IN_Y, src}, none, {IN_Y, 1 - src}, 0.f, 0.f, two(exp_out - exp_z - exp_y)};
+      if (k + length < count) plan->stages.push_back({apply});
+      else plan->last = apply;
+      src = 1 - src;
+      k += length;
+    };
+    if (mode == SMALL) {
+      od::NsSteps list = {};
+      list.count = length;
+      for (int l = 0; l < length; ++l) {
+        const Step& st = steps[k + l];
+        list.a[l] = (float)st.a; list.b[l] = (float)st.b; list.c[l] = (float)st.c;
+        list.s[l] = two(exponent_for(st.top * st.top));
+        list.p[l] = two(exponent_for(st.poly));
+        list.t[l] = two(exponent_for(st.poly * st.top * st.top));
+        list.z[l] = two(exponent_for(product_bound(steps, k, l + 1)));
+      }
+      plan->stages.push_back({PlannedJob{od::NS_GRAM, {IN_Y, src}, {IN_Y, src}, none, partials, 0.f, 0.f, 1.f}});
+      plan->stages.push_back({PlannedJob{od::NS_SMALL, partials, none, none, s_mat, 0.f, 0.f, two(-2 * exp_y)}});
+      plan->steps.push_back(list);
+      apply_of(s_mat, exponent_for(product_bound(steps, k, length)));
+      continue;
+    }
     // P and Z change between the matrices behind S and T (step by step: P alone, where T would be)
-    int free_mats[3] = {2, 3, 4};
-    Operand p_mat = length > 1 ? Operand{false, free_mats[0]} : t_mat, z_mat = p_mat;
+    Operand p_mat = length > 1 ? Operand{IN_SYMMETRIC, 2} : t_mat, z_mat = p_mat;
     if (length > 1) plan->symmetric = kMostSymmetric;
     int exp_s = exponent_for(steps[k].top * steps[k].top), exp_p = exponent_for(steps[k].poly), exp_z = exp_p;
-    plan->stages.push_back({PlannedJob{od::NS_GRAM, {true, src}, {true, src}, none, s_mat, 0.f, 0.f, two(exp_s - 2 * exp_y)}});
+    plan->stages.push_back({PlannedJob{od::NS_GRAM, {IN_Y, src}, {IN_Y, src}, none, split ? partials : s_mat, 0.f, 0.f, two(exp_s - 2 * exp_y)}});
+    if (split) plan->stages.push_back({PlannedJob{od::NS_REDUCE, partials, none, none, s_mat, 0.f, 0.f, two(exp_s - 2 * exp_y)}});
     auto poly = [&](const Step& st, Operand out) {
       return PlannedJob{od::NS_SYM, s_mat, s_mat, s_mat, out, (float)(st.a * two(exp_p)), (float)(st.b * two(exp_p - exp_s)), (float)(st.c * two(exp_p - 2 * exp_s))};
     };
@@ -178,8 +229,8 @@ static void plan_jobs(const std::vector<Step>& steps, bool segmented, Plan* plan
       Operand new_z = z_mat;
       if (l > 1) {
         const int exp_new = exponent_for(product_bound(steps, k, l));
-        new_z = Operand{false, 2 + 3 + 4 - p_mat.index - z_mat.index};
-        pair.push_back(PlannedJob{od::NS_SYM, p_mat, z_mat, none, new_z, 0.f, 0.f, two(exp_new - exp_p - exp_z)});
+        new_z = Operand{IN_SYMMETRIC, 2 + 3 + 4 - p_mat.index - z_mat.index};
+        pair.push_back(PlannedJob{od::NS_FULL, p_mat, z_mat, none, new_z, 0.f, 0.f, two(exp_new - exp_p - exp_z)});
         exp_z = exp_new;
       }
       plan->stages.push_back(pair);
@@ -192,22 +243,19 @@ static void plan_jobs(const std::vector<Step>& steps, bool segmented, Plan* plan
       exp_p = exponent_for(st.poly);
       int index = 2;
       while (index == z_mat.index) ++index;
-      p_mat = Operand{false, index};
+      p_mat = Operand{IN_SYMMETRIC, index};
       plan->stages.push_back({poly(st, p_mat)});
     }
     if (length > 1) {
       const int exp_new = exponent_for(product_bound(steps, k, length));
-      const Operand new_z{false, 2 + 3 + 4 - p_mat.index - z_mat.index};
-      plan->stages.push_back({PlannedJob{od::NS_SYM, p_mat, z_mat, none, new_z, 0.f, 0.f, two(exp_new - exp_p - exp_z)}});
+      const Operand new_z{IN_SYMMETRIC, 2 + 3 + 4 - p_mat.index - z_mat.index};
+      // not mirrored: the two orders of the rounded factors differ by their commutator, and one triangle of each would
+      // leave more than either (1528 x 3304, cut 2 + 2 + 1: 1.54e-3 mirrored, 1.34e-3 not)
+      plan->stages.push_back({PlannedJob{od::NS_FULL, p_mat, z_mat, none, new_z, 0.f, 0.f, two(exp_new - exp_p - exp_z)}});
       z_mat = new_z;
       exp_z = exp_new;
     }
-    k += length;
-    const int exp_out = k < count ? exponent_for(steps[k].top) : 0;
-    const PlannedJob apply{od::NS_APPLY, z_mat, {true, src}, none, {true, 1 - src}, 0.f, 0.f, two(exp_out - exp_z - exp_y)};
-    if (k < count) plan->stages.push_back({apply});
-    else plan->last = apply;
-    src = 1 - src;
+    apply_of(z_mat, exp_z);
   }
 }
 
@@ -242,12 +290,12 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
   h->cfg = *cfg;
   std::vector<Step> steps;
   if ((rc = plan_steps(*cfg, &steps)) != ORTHDION_OK) return rc;
-  plan_jobs(steps, false, &h->step_by_step);
-  plan_jobs(steps, true, &h->segments);
   h->first_exp = exponent_for(steps[0].top);
   const bool exact = cfg->precision == ORTHDION_PREC_EXACT ||
                      (cfg->precision == ORTHDION_PREC_AUTO && !(cfg->x_dtype == ORTHDION_BF16 && cfg->g_dtype == ORTHDION_BF16));
   h->parts = exact ? 2 : 1;
+  for (int split = 0; split < 2; ++split)
+    for (int mode = 0; mode < kModes; ++mode) plan_jobs(steps, (Mode)mode, split != 0, h->parts, &h->plans[split][mode]);
 
   // classes in order of first appearance
   struct Shape { int p, q, tall; std::vector<int> members; };
@@ -265,8 +313,10 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
   for (const Shape& c : classes) {
     const int64_t elements = (int64_t)c.p * c.q;
     const int lp = pitch(c.p), lq = pitch(c.q);
-    const Plan& plan = takes_segments(c.p, c.q) ? h->segments : h->step_by_step;
-    const int64_t stride = h->parts * (2 * od::ns_y_plane(c.p, lq) + plan.symmetric * od::ns_s_plane(c.p, lp));
+    const Mode mode = mode_for(c.p, c.q);
+    const int splits = splits_for(mode, c.p, c.q, (int)c.members.size(), h->parts);
+    const Plan& plan = h->plans[splits > 0][mode];
+    const int64_t stride = h->parts * (2 * od::ns_y_plane(c.p, lq) + plan.symmetric * od::ns_s_plane(c.p, lp)) + od::ns_partials(c.p, splits);
     for (size_t done = 0; done < c.members.size();) {
       if (h->clusters.empty() || held + elements > kClusterElements || (int)h->clusters.back().classes.size() == od::kNsClasses) {
         h->clusters.push_back(Cluster{});
@@ -282,7 +332,7 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
       job.p = c.p; job.q = c.q; job.lp = lp; job.lq = lq; job.nb = take; job.tall = c.tall;
       job.mat0 = (int)h->order.size();
       job.stride = stride;
-      cl.classes.push_back(Class{job, slices, &plan});
+      cl.classes.push_back(Class{job, slices, &plan, splits});
       slices = align_up(slices + (size_t)take * (size_t)stride * 2);
       most = std::max(most, slices);
       for (int k = 0; k < take; ++k) {
@@ -348,12 +398,13 @@ static int muon_run(orthdion_muon_handle h, void* const* X, const void* const* G
       j = c.job;
       j.base = reinterpret_cast<uint16_t*>(ws + h->off_slices + c.offset);
       auto at = [&](const Operand& o) {
-        const int64_t y = od::ns_y_plane(j.p, j.lq) * parts;
-        return o.y ? o.index * y : 2 * y + o.index * od::ns_s_plane(j.p, j.lp) * parts;
+        const int64_t y = od::ns_y_plane(j.p, j.lq) * parts, s = od::ns_s_plane(j.p, j.lp) * parts;
+        return o.where == IN_Y ? o.index * y : 2 * y + (o.where == IN_SYMMETRIC ? o.index : c.plan->symmetric) * s;
       };
       j.kind = job.kind;
       j.a = at(job.a); j.b = at(job.b); j.e = at(job.e); j.out = at(job.out);
       j.ca = job.ca; j.cb = job.cb; j.cc = job.cc;
+      j.splits = job.kind == od::NS_GRAM || job.kind == od::NS_REDUCE || job.kind == od::NS_SMALL ? c.splits : 0;
     };
     OD_TRY(od::launch_muon_begin(entries.get() + cl.mat0, h->table.data() + cl.mat0, cl.mat0, cl.count, t, h->cfg.mu, nesterov, gbf, st));
     args.count = 0;
@@ -364,12 +415,24 @@ static int muon_run(orthdion_muon_handle h, void* const* X, const void* const* G
     }
     OD_TRY(od::launch_muon_scale(args, t, h->cfg.mu, nesterov, gbf, parts, h->cfg.eps, std::ldexp(1.0, h->first_exp), st));
     const NsArgs last = args;
-    for (size_t s = 0; s < stages; ++s) {
+    // the jobs of stage s that `of` takes; the plan of the last of them
+    auto gather = [&](size_t s, auto&& of) {
+      const Plan* plan = nullptr;
       args.count = 0;
       for (const Class& c : cl.classes)
         if (s < c.plan->stages.size())
-          for (const PlannedJob& job : c.plan->stages[s]) add(c, job);
-      OD_TRY(od::launch_ns_products(args, parts, st));
+          for (const PlannedJob& job : c.plan->stages[s])
+            if (of(job.kind)) {
+              add(c, job);
+              plan = c.plan;
+            }
+      return plan;
+    };
+    for (size_t s = 0; s < stages; ++s) {
+      if (gather(s, [](od::NsKind k) { return k <= od::NS_FULL; })) OD_TRY(od::launch_ns_products(args, parts, st));
+      if (gather(s, [](od::NsKind k) { return k == od::NS_REDUCE; })) OD_TRY(od::launch_ns_reduce(args, parts, st));
+      // small matrices take three stages a segment
+      if (const Plan* plan = gather(s, [](od::NsKind k) { return k == od::NS_SMALL; })) OD_TRY(od::launch_ns_small(args, plan->steps[s / 3], parts, st));
     }
     OD_TRY(od::launch_ns_final(last, t, parts, update, keep, h->cfg.lr, xbf, st));
   }
