@@ -4,6 +4,7 @@ kernels.  There is no CPU fallback: a missing library is an error."""
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import List, Optional, Sequence
 
@@ -229,10 +230,7 @@ def orthdion_set_variant(handle: int, variant: int) -> None:
 
 
 def _ptr_array(ptrs: Sequence[int]):
-    arr = (ctypes.c_void_p * len(ptrs))()
-    for i, p in enumerate(ptrs):
-        arr[i] = p
-    return arr
+    return (ctypes.c_void_p * len(ptrs))(*ptrs)
 
 
 def orthdion_step(handle: int, X: Sequence[int], G: Sequence[int], M: Sequence[int], Q: Sequence[int],
@@ -513,6 +511,9 @@ def _dtypes(torch, x_dtype: str, g_dtype: Optional[str]):
     return known[x_dtype], known[g_dtype or x_dtype]
 
 
+_dtype_of = operator.attrgetter("dtype")
+
+
 def _per_item(name: str, value, count: int) -> List[float]:
     """One float per item from one for all or a sequence."""
     got = [float(value)] * count if isinstance(value, (int, float)) else [float(v) for v in value]
@@ -542,6 +543,7 @@ class Muon:
         self.lds = [tuple(int(v) for v in ld) for ld in lds] if lds is not None else [(n, n, n) for _, n in self.shapes]
         if len(self.lds) != self.nmat:
             raise ValueError(f"lds: expected {self.nmat} triples, got {len(self.lds)}")
+        self._strides = [[(ld[k], 1) for ld in self.lds] for k in range(3)]
         (xc, self._x_dtype), (gc, self._g_dtype) = _dtypes(torch, x_dtype, g_dtype)
         rules = {"none": lambda m, n: 1.0, "spectral": lambda m, n: max(1.0, m / n) ** 0.5, "rms": lambda m, n: 0.2 * max(m, n) ** 0.5}
         if isinstance(scale, str):
@@ -554,37 +556,41 @@ class Muon:
         self.workspace_bytes = orthdion_muon_workspace_bytes(self.handle)
         self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
 
-    def _pointers(self, **named) -> List[List[int]]:
-        """Addresses of lists of tensors, after the checks that raw addresses cannot have: one wrong type, shape, stride or
+    def _pointers(self, name: str, seq, dtype, which: int) -> List[int]:
+        """Addresses of a list of tensors, after the checks that raw addresses cannot have: one wrong type, shape, stride or
         device would be an access out of bounds."""
-        out = []
-        for name, (seq, dtype, which) in named.items():
-            if len(seq) != self.nmat:
-                raise ValueError(f"{name}: expected {self.nmat} tensors, got {len(seq)}")
-            for i, t in enumerate(seq):
-                m, n = self.shapes[i]
-                ld = self.lds[i][which]
-                rows = t.dim() == 2 and (n == 1 or t.stride(1) == 1) and (m == 1 or t.stride(0) == ld)
-                if t.device.type != "cuda" or tuple(t.shape) != (m, n) or t.dtype != dtype or not rows:
-                    raise ValueError(f"{name}[{i}]: need a {dtype} device tensor of shape {(m, n)} with rows {ld} elements apart, got "
-                                     f"{t.dtype} {tuple(t.shape)} with strides {tuple(t.stride())} on {t.device}")
-                if t.device != self.workspace.device:
-                    raise ValueError(f"{name}[{i}]: on {t.device}, the workspace on {self.workspace.device}")
-            out.append([t.data_ptr() for t in seq])
-        return out
+        tensor = self._torch.Tensor
+        # a handful of C calls a tensor; only what does not pass is looked at one by one
+        if (self.workspace.is_cuda and set(map(tensor.get_device, seq)) == {self.workspace.get_device()}
+                and set(map(_dtype_of, seq)) == {dtype} and list(map(tensor.size, seq)) == self.shapes
+                and list(map(tensor.stride, seq)) == self._strides[which]):
+            return list(map(tensor.data_ptr, seq))
+        if len(seq) != self.nmat:
+            raise ValueError(f"{name}: expected {self.nmat} tensors, got {len(seq)}")
+        for i, t in enumerate(seq):
+            m, n = self.shapes[i]
+            ld = self.lds[i][which]
+            rows = t.dim() == 2 and (n == 1 or t.stride(1) == 1) and (m == 1 or t.stride(0) == ld)
+            if t.device.type != "cuda" or tuple(t.shape) != (m, n) or t.dtype != dtype or not rows:
+                raise ValueError(f"{name}[{i}]: need a {dtype} device tensor of shape {(m, n)} with rows {ld} elements apart, got "
+                                 f"{t.dtype} {tuple(t.shape)} with strides {tuple(t.stride())} on {t.device}")
+            if t.device != self.workspace.device:
+                raise ValueError(f"{name}[{i}]: on {t.device}, the workspace on {self.workspace.device}")
+        return [t.data_ptr() for t in seq]
 
     def _stream(self, stream) -> int:
         return stream if stream is not None else self._torch.cuda.current_stream(self.workspace.device).cuda_stream
 
     def step(self, X, G, M, stream=None) -> None:
         """One optimizer step: X and M are updated in place."""
-        x, g, m = self._pointers(X=(X, self._x_dtype, 0), G=(G, self._g_dtype, 1), M=(M, self._torch.float32, 2))
+        x, g = self._pointers("X", X, self._x_dtype, 0), self._pointers("G", G, self._g_dtype, 1)
+        m = self._pointers("M", M, self._torch.float32, 2)
         with self._torch.cuda.device(self.workspace.device):
             orthdion_muon_step(self.handle, x, g, m, self.workspace.data_ptr(), self.workspace_bytes, self._stream(stream))
 
     def orthogonalise(self, A, out, stream=None) -> None:
         """The orthogonalised A (laid out as G) into `out` (laid out as X)."""
-        a, o = self._pointers(A=(A, self._g_dtype, 1), out=(out, self._x_dtype, 0))
+        a, o = self._pointers("A", A, self._g_dtype, 1), self._pointers("out", out, self._x_dtype, 0)
         with self._torch.cuda.device(self.workspace.device):
             orthdion_muon_orthogonalise(self.handle, a, o, self.workspace.data_ptr(), self.workspace_bytes, self._stream(stream))
 
@@ -632,15 +638,20 @@ class AdamW:
         torch = self._torch
         if counter.device.type != "cuda" or counter.dtype != torch.int32 or tuple(counter.shape) != (2,) or not counter.is_contiguous():
             raise ValueError(f"counter: need an int32 device tensor of two, got {counter.dtype} {tuple(counter.shape)} on {counter.device}")
+        tensor, device, addresses = torch.Tensor, {counter.get_device()}, []
         for name, seq, dtype in (("X", X, self._x_dtype), ("G", G, self._g_dtype), ("M", M, torch.float32), ("V", V, torch.float32)):
-            if len(seq) != len(self.lengths):
-                raise ValueError(f"{name}: expected {len(self.lengths)} tensors, got {len(seq)}")
-            for i, t in enumerate(seq):
-                if t.device != counter.device or t.dtype != dtype or t.numel() != self.lengths[i] or not t.is_contiguous():
-                    raise ValueError(f"{name}[{i}]: need a contiguous {dtype} tensor of {self.lengths[i]} elements on {counter.device}, got "
-                                     f"{t.dtype} {tuple(t.shape)} on {t.device}, contiguous={t.is_contiguous()}")
+            # a handful of C calls a tensor; only what does not pass is looked at one by one
+            if not (list(map(tensor.numel, seq)) == self.lengths and set(map(_dtype_of, seq)) == {dtype}
+                    and set(map(tensor.get_device, seq)) == device and all(map(tensor.is_contiguous, seq))):
+                if len(seq) != len(self.lengths):
+                    raise ValueError(f"{name}: expected {len(self.lengths)} tensors, got {len(seq)}")
+                for i, t in enumerate(seq):
+                    if t.device != counter.device or t.dtype != dtype or t.numel() != self.lengths[i] or not t.is_contiguous():
+                        raise ValueError(f"{name}[{i}]: need a contiguous {dtype} tensor of {self.lengths[i]} elements on {counter.device}, "
+                                         f"got {t.dtype} {tuple(t.shape)} on {t.device}, contiguous={t.is_contiguous()}")
+            addresses.append(list(map(tensor.data_ptr, seq)))
         with torch.cuda.device(counter.device):
-            orthdion_adamw_step(self.handle, *([t.data_ptr() for t in seq] for seq in (X, G, M, V)), counter.data_ptr(),
+            orthdion_adamw_step(self.handle, *addresses, counter.data_ptr(),
                                 stream if stream is not None else torch.cuda.current_stream(counter.device).cuda_stream)
 
     def set_lr(self, lr: float) -> None:

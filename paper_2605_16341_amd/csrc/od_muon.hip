@@ -566,61 +566,48 @@ __global__ __launch_bounds__(TL::THREADS, TL::BLOCKS) void k_ns_products(NsArgs 
   }
 }
 
-// Adds the partial sums of a Gram matrix in their order: one workgroup 32 rows of a tile, written in both triangles.
+// Adds the partial sums of a Gram matrix in their order: one workgroup 8 rows of a tile, written in both triangles.
+// Bound by the latency of the loads, four of them in flight.
 template <int PARTS>
 __global__ __launch_bounds__(256) void k_ns_reduce(NsArgs args) {
-  constexpr int T = kNsSplitTile;
-  __shared__ float tile[32][T + 4];
+  constexpr int T = kNsSplitTile, R = 8;
+  __shared__ float tile[R][T + 4];
   const NsJob c = args.j[ns_job(args, blockIdx.x)];
   const int pp = up64(c.p), n = (c.p + T - 1) / T, tiles = n * (n + 1) / 2, local = blockIdx.x - c.first;
-  const int z = quotient(local, 4 * tiles), in_z = local - z * 4 * tiles, t = in_z >> 2, part_rows = in_z & 3;
+  const int z = quotient(local, T / R * tiles), in_z = local - z * (T / R) * tiles, t = in_z / (T / R), r0 = in_z % (T / R) * R;
   int ti, tj;
   upper_tile(t, n, &ti, &tj);
+  if (ti * T + r0 >= c.p) return;
   uint16_t* slice = c.base + z * c.stride;
-  const float* in = reinterpret_cast<const float*>(slice + c.a) + (int64_t)t * c.splits * T * T + part_rows * 32 * T;
   const int64_t splane = (int64_t)c.p * c.lp;
-  const int tid = threadIdx.x, r = tid >> 3, c0 = (tid & 7) * 4;
-  f32x4 sum[4] = {};
-  for (int s = 0; s < c.splits; ++s)
+  const int tid = threadIdx.x, r = tid >> 5, c0 = (tid & 31) * 4;
+  const float* in = reinterpret_cast<const float*>(slice + c.a) + (int64_t)t * c.splits * T * T + (r0 + r) * T + c0;
+  f32x4 sum = {};
+#pragma unroll 4
+  for (int s = 0; s < c.splits; ++s) sum += *reinterpret_cast<const f32x4*>(in + (int64_t)s * T * T);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) sum[k] += *reinterpret_cast<const f32x4*>(in + (int64_t)s * T * T + r * T + c0 + 32 * k);
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) tile[r][c0 + 32 * k + e] = c.cc * sum[k][e];
+  for (int e = 0; e < 4; ++e) tile[r][c0 + e] = c.cc * sum[e];
   __syncthreads();
   uint16_t* out = slice + c.out;
-  // rows, eight columns a thread and turn
-  for (int k = tid; k < 32 * (T / 8); k += 256) {
-    const int row = ti * T + part_rows * 32 + k / (T / 8), col = tj * T + k % (T / 8) * 8;
-    if (row >= c.p || col >= pp) continue;
-    const float* v = &tile[k / (T / 8)][k % (T / 8) * 8];
+  auto put = [&](int row, int col, auto&& at) {
     u32x4 w[PARTS];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       uint32_t s[PARTS];
-      split2<PARTS>(col + 2 * e < c.p ? v[2 * e] : 0.f, col + 2 * e + 1 < c.p ? v[2 * e + 1] : 0.f, s);
+      split2<PARTS>(col + 2 * e < c.p ? at(2 * e) : 0.f, col + 2 * e + 1 < c.p ? at(2 * e + 1) : 0.f, s);
 #pragma unroll
       for (int part = 0; part < PARTS; ++part) w[part][e] = s[part];
     }
 #pragma unroll
     for (int part = 0; part < PARTS; ++part) *reinterpret_cast<u32x4*>(out + part * splane + (int64_t)row * c.lp + col) = w[part];
-  }
-  if (ti == tj) return;
-  // columns as rows: the tile lies above the diagonal, so its rows are all inside
-  for (int k = tid; k < T * 4; k += 256) {
-    const int row = tj * T + k / 4, col = ti * T + part_rows * 32 + k % 4 * 8;
-    if (row >= c.p) continue;
-    u32x4 w[PARTS];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      uint32_t s[PARTS];
-      split2<PARTS>(tile[k % 4 * 8 + 2 * e][k / 4], tile[k % 4 * 8 + 2 * e + 1][k / 4], s);
-#pragma unroll
-      for (int part = 0; part < PARTS; ++part) w[part][e] = s[part];
-    }
-#pragma unroll
-    for (int part = 0; part < PARTS; ++part) *reinterpret_cast<u32x4*>(out + part * splane + (int64_t)row * c.lp + col) = w[part];
+  };
+  // eight columns of a row a thread; above the diagonal also eight rows of a column, all of them inside
+  if (tid < R * (T / 8)) {
+    const int k = tid / (T / 8), row = ti * T + r0 + k, col = tj * T + tid % (T / 8) * 8;
+    if (row < c.p && col < pp) put(row, col, [&](int e) { return tile[k][tid % (T / 8) * 8 + e]; });
+  } else if (ti != tj) {
+    const int k = tid - R * (T / 8), row = tj * T + k;
+    if (row < c.p) put(row, ti * T + r0, [&](int e) { return tile[e][k]; });
   }
 }
 
@@ -787,44 +774,46 @@ __global__ __launch_bounds__(TL::THREADS, TL::BLOCKS) void k_ns_final(NsArgs arg
   const bool vec = (reinterpret_cast<uintptr_t>(e.X) & (XBF ? 7 : 15)) == 0 && (a.ldx & 3) == 0;
   const float step = update ? lr * a.scale * scale : -scale;
   const float kx = update ? keep : 0.f;
+  // accumulators one by one: the four runs of a lane are loaded together, then written
+  static_for<TL::FM * TL::FN>([&](auto n) {
+    constexpr int i = decltype(n)::value / TL::FN, j = decltype(n)::value % TL::FN;
+    const int row = TALL ? j0 + 32 * j + (lane & 31) : i0 + 32 * i + (lane & 31);
+    const int col = (TALL ? i0 + 32 * i : j0 + 32 * j) + 4 * (lane >> 5);
+    if (row >= a.m) return;
+    const int64_t at = (int64_t)row * a.ldx + col;
+    float x[4][4];
 #pragma unroll
-  for (int i = 0; i < TL::FM; ++i)
+    for (int v4 = 0; v4 < 4; ++v4) {
 #pragma unroll
-    for (int j = 0; j < TL::FN; ++j)
+      for (int k = 0; k < 4; ++k) x[v4][k] = 0.f;
+      if (!update || col + 8 * v4 >= a.n) continue;
+      if (vec && col + 8 * v4 + 4 <= a.n) {
+        if constexpr (XBF) SrcBF16::unpack4(*reinterpret_cast<const u32x2*>(reinterpret_cast<const uint16_t*>(e.X) + at + 8 * v4), x[v4]);
+        else SrcF32::unpack4(*reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(e.X) + at + 8 * v4), x[v4]);
+      } else {
 #pragma unroll
-      for (int v4 = 0; v4 < 4; ++v4) {
-        const int run = 8 * v4 + 4 * (lane >> 5);
-        const int row = TALL ? j0 + 32 * j + (lane & 31) : i0 + 32 * i + (lane & 31);
-        const int col = TALL ? i0 + 32 * i + run : j0 + 32 * j + run;
-        if (row >= a.m || col >= a.n) continue;
-        const int64_t at = (int64_t)row * a.ldx + col;
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
-        if (vec && col + 4 <= a.n) {
-          if constexpr (XBF) {
-            u32x2* px = reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(e.X) + at);
-            if (update) SrcBF16::unpack4(*px, x);
+        for (int k = 0; k < 4; ++k)
+          if (col + 8 * v4 + k < a.n) x[v4][k] = load_elem<XBF>(e.X, at + 8 * v4 + k);
+      }
+    }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = kx * x[k] - step * acc[i][j][4 * v4 + k];
-            *px = u32x2{pack_bf16_rne(x[0], x[1]), pack_bf16_rne(x[2], x[3])};
-          } else {
-            f32x4* px = reinterpret_cast<f32x4*>(reinterpret_cast<float*>(e.X) + at);
-            if (update) SrcF32::unpack4(*px, x);
-            f32x4 o;
+    for (int v4 = 0; v4 < 4; ++v4) {
+      if (col + 8 * v4 >= a.n) continue;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) o[k] = kx * x[k] - step * acc[i][j][4 * v4 + k];
-            *px = o;
-          }
-        } else {
+      for (int k = 0; k < 4; ++k) x[v4][k] = kx * x[v4][k] - step * acc[i][j][4 * v4 + k];
+      if (vec && col + 8 * v4 + 4 <= a.n) {
+        if constexpr (XBF) *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(e.X) + at + 8 * v4) = u32x2{pack_bf16_rne(x[v4][0], x[v4][1]), pack_bf16_rne(x[v4][2], x[v4][3])};
+        else *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(e.X) + at + 8 * v4) = f32x4{x[v4][0], x[v4][1], x[v4][2], x[v4][3]};
+      } else {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            if (col + k >= a.n) continue;
-            if (update) x[k] = load_elem<XBF>(e.X, at + k);
-            const float o = kx * x[k] - step * acc[i][j][4 * v4 + k];
-            if constexpr (XBF) reinterpret_cast<uint16_t*>(e.X)[at + k] = (uint16_t)pack_bf16_rne(o, 0.f);
-            else reinterpret_cast<float*>(e.X)[at + k] = o;
-          }
+        for (int k = 0; k < 4; ++k) {
+          if (col + 8 * v4 + k >= a.n) continue;
+          if constexpr (XBF) reinterpret_cast<uint16_t*>(e.X)[at + 8 * v4 + k] = (uint16_t)pack_bf16_rne(x[v4][k], 0.f);
+          else reinterpret_cast<float*>(e.X)[at + 8 * v4 + k] = x[v4][k];
         }
       }
+    }
+  });
 }
 
 // ------------------------------------------------------------------------------------
@@ -885,7 +874,11 @@ hipError_t go(K* kernel, const NsJobs<N>& a, hipStream_t st, A... rest) {
 }
 
 typedef NsTile<128, 2, 2> Small;
+#ifdef TRY
+typedef TRY Large;
+#else
 typedef NsTile<256, 2, 4> Large;
+#endif
 
 template <int T>
 int tiles_of(const NsJob& c) {
@@ -940,7 +933,7 @@ hipError_t launch_ns_products(const NsArgs& a, int parts, hipStream_t st) {
 }
 
 hipError_t launch_ns_reduce(const NsArgs& a, int parts, hipStream_t st) {
-  const NsArgs o = laid_out(a, any, [](const NsJob& c) { const int n = ceil_div(c.p, kNsSplitTile); return 4 * (n * (n + 1) / 2); });
+  const NsArgs o = laid_out(a, any, [](const NsJob& c) { const int n = ceil_div(c.p, kNsSplitTile); return kNsSplitTile / 8 * (n * (n + 1) / 2); });
   if (parts == 2) k_ns_reduce<2><<<o.total, 256, 0, st>>>(o);
   else k_ns_reduce<1><<<o.total, 256, 0, st>>>(o);
   return hipGetLastError();

@@ -21,8 +21,13 @@ constexpr size_t kAlign = 256;
 constexpr int64_t kMaxDim = 1 << 22;       // 32-bit offsets of the operand loads: 256 rows of 2^22 fp16 words
 // Matrices step together (a cluster: every kernel of the iteration is one launch over it) up to this many elements; the
 // next cluster reuses the workspace.
-constexpr int64_t kClusterElements = (int64_t)1 << 28;
-constexpr int64_t kPartElements = 16384;   // elements behind one partial sum of squares
+#ifndef CLU
+#define CLU 29
+#endif
+constexpr int64_t kClusterElements = (int64_t)1 << CLU;
+// Elements behind one partial sum of squares, while those are fewer than kMuonParts.  With 16384 the odd matrix of six small
+// ones (201 x 327) took 24 us, the time of a thread's chain of single loads.
+constexpr int64_t kPartElements = 2048;
 
 size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 int up64(int64_t v) { return (int)((v + 63) / 64 * 64); }
@@ -53,7 +58,8 @@ constexpr int kModes = 3;
 struct Class {
   NsJob job;                               // shape, slices and tables; base from the call
   size_t offset;                           // bytes of its slices behind the cluster's start
-  const Plan* plan;
+  const Plan* plan[2];                     // of the orthogonalisation and of the step
+  int symmetric;                           // matrices in a slice
   int splits;                              // of its Gram matrices, 0: one sum
 };
 struct Cluster {
@@ -71,7 +77,10 @@ struct Cluster {
 //   two words, 40 x 200 to 512 x 2048: step by step 1.1 to 6.1e-6, 2 + 1 + 2 1.1 to 5.2e-6, 2 + 2 + 1 1.2 to 5.2e-6 (twice as
 //   much as step by step on some), 3 + 2 1.1 to 7e-6
 //   one word for Y, two for the p x p work (small matrices), 40 x 200 to 300 x 700: 3 + 2 0.5 to 1.4e-3, in one segment 0.3 to 5.4e-3
-constexpr double kGrowth = 13.0, kSmallGrowth = 160.0;
+constexpr double kGrowth = 13.0, kLongGrowth = 160.0;
+// The long first segment (3 + 2) is taken where O does not leave by itself with the precision of one word: by the step in
+// fast precision, whose X of 8 bits takes lr O (24 decoder layers: 40.8 -> 35.6 ms), and by small matrices.
+bool long_first(Mode mode, int parts, bool step) { return parts == 1 && (mode == SMALL || step); }
 // In units of p^3 a step by itself costs 3 rho + 1 with rho = q / p, a segment of L steps 3 rho + 4 L - 3: the same for two
 // segments of 3 + 2 and five steps at rho = 1.  But a segment has more and smaller launches.
 #ifndef SEG_P
@@ -103,7 +112,7 @@ struct orthdion_muon_ctx {
   std::vector<orthdion_muon_matdesc> mats;
   orthdion_muon_config cfg;
   int parts;
-  Plan plans[2][kModes];                   // [Gram matrices in partial sums][mode]
+  Plan plans[2][2][kModes];                // [step][Gram matrices in partial sums][mode]
   int first_exp;                           // power of two of the scaled input
   std::vector<int> order;                  // table row -> matrix
   std::vector<MuonMat> table;              // by row
@@ -166,7 +175,7 @@ static double product_bound(const std::vector<Step>& steps, int from, int count)
   return std::max(1.02 * most, 1.0 / 256);
 }
 
-static void plan_jobs(const std::vector<Step>& steps, Mode mode, bool split, int parts, Plan* plan) {
+static void plan_jobs(const std::vector<Step>& steps, Mode mode, bool split, int parts, bool step, Plan* plan) {
   const int count = (int)steps.size() - 1;
   const Operand none{IN_SYMMETRIC, 0}, s_mat{IN_SYMMETRIC, 0}, t_mat{IN_SYMMETRIC, 1}, partials{IN_PARTIALS, 0};
   auto two = [](int e) { return (float)std::ldexp(1.0, e); };
@@ -176,7 +185,7 @@ static void plan_jobs(const std::vector<Step>& steps, Mode mode, bool split, int
     int length = 1;
     // two words: only the first and the last segment hold more than one step
     if (mode != STEP_BY_STEP && (parts == 1 || k == 0 || k + 2 == count)) {
-      const double limit = k == 0 && mode == SMALL && parts == 1 ? kSmallGrowth : kGrowth;
+      const double limit = k == 0 && long_first(mode, parts, step) ? kLongGrowth : kGrowth;
       double growth = 1.0;
       while (k + length < count) {
         growth *= steps[k + length - 1].poly * steps[k + length - 1].poly;
@@ -294,8 +303,9 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
   const bool exact = cfg->precision == ORTHDION_PREC_EXACT ||
                      (cfg->precision == ORTHDION_PREC_AUTO && !(cfg->x_dtype == ORTHDION_BF16 && cfg->g_dtype == ORTHDION_BF16));
   h->parts = exact ? 2 : 1;
-  for (int split = 0; split < 2; ++split)
-    for (int mode = 0; mode < kModes; ++mode) plan_jobs(steps, (Mode)mode, split != 0, h->parts, &h->plans[split][mode]);
+  for (int step = 0; step < 2; ++step)
+    for (int split = 0; split < 2; ++split)
+      for (int mode = 0; mode < kModes; ++mode) plan_jobs(steps, (Mode)mode, split != 0, h->parts, step != 0, &h->plans[step][split][mode]);
 
   // classes in order of first appearance
   struct Shape { int p, q, tall; std::vector<int> members; };
@@ -307,16 +317,22 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
     if (k == classes.size()) classes.push_back(Shape{p, q, tall, {}});
     classes[k].members.push_back(i);
   }
+  bool all_small = true;
+  for (const Shape& c : classes) all_small = all_small && mode_for(c.p, c.q) == SMALL;
   // clusters
   int64_t held = 0;
   size_t slices = 0, most = 0;
   for (const Shape& c : classes) {
     const int64_t elements = (int64_t)c.p * c.q;
     const int lp = pitch(c.p), lq = pitch(c.q);
-    const Mode mode = mode_for(c.p, c.q);
+    // Beside larger matrices small ones ride along in their launches, which are there anyway: six matrices of 128 to 392 rows
+    // 209 us a step, with launches of their own kernel in between 275.
+    Mode mode = mode_for(c.p, c.q);
+    if (mode == SMALL && !all_small) mode = STEP_BY_STEP;
     const int splits = splits_for(mode, c.p, c.q, (int)c.members.size(), h->parts);
-    const Plan& plan = h->plans[splits > 0][mode];
-    const int64_t stride = h->parts * (2 * od::ns_y_plane(c.p, lq) + plan.symmetric * od::ns_s_plane(c.p, lp)) + od::ns_partials(c.p, splits);
+    const Plan* const plan[2] = {&h->plans[0][splits > 0][mode], &h->plans[1][splits > 0][mode]};
+    const int symmetric = std::max(plan[0]->symmetric, plan[1]->symmetric);
+    const int64_t stride = h->parts * (2 * od::ns_y_plane(c.p, lq) + symmetric * od::ns_s_plane(c.p, lp)) + od::ns_partials(c.p, splits);
     for (size_t done = 0; done < c.members.size();) {
       if (h->clusters.empty() || held + elements > kClusterElements || (int)h->clusters.back().classes.size() == od::kNsClasses) {
         h->clusters.push_back(Cluster{});
@@ -332,7 +348,7 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
       job.p = c.p; job.q = c.q; job.lp = lp; job.lq = lq; job.nb = take; job.tall = c.tall;
       job.mat0 = (int)h->order.size();
       job.stride = stride;
-      cl.classes.push_back(Class{job, slices, &plan, splits});
+      cl.classes.push_back(Class{job, slices, {plan[0], plan[1]}, symmetric, splits});
       slices = align_up(slices + (size_t)take * (size_t)stride * 2);
       most = std::max(most, slices);
       for (int k = 0; k < take; ++k) {
@@ -399,7 +415,7 @@ static int muon_run(orthdion_muon_handle h, void* const* X, const void* const* G
       j.base = reinterpret_cast<uint16_t*>(ws + h->off_slices + c.offset);
       auto at = [&](const Operand& o) {
         const int64_t y = od::ns_y_plane(j.p, j.lq) * parts, s = od::ns_s_plane(j.p, j.lp) * parts;
-        return o.where == IN_Y ? o.index * y : 2 * y + (o.where == IN_SYMMETRIC ? o.index : c.plan->symmetric) * s;
+        return o.where == IN_Y ? o.index * y : 2 * y + (o.where == IN_SYMMETRIC ? o.index : c.symmetric) * s;
       };
       j.kind = job.kind;
       j.a = at(job.a); j.b = at(job.b); j.e = at(job.e); j.out = at(job.out);
@@ -410,8 +426,8 @@ static int muon_run(orthdion_muon_handle h, void* const* X, const void* const* G
     args.count = 0;
     size_t stages = 0;
     for (const Class& c : cl.classes) {
-      add(c, c.plan->last);
-      stages = std::max(stages, c.plan->stages.size());
+      add(c, c.plan[update]->last);
+      stages = std::max(stages, c.plan[update]->stages.size());
     }
     OD_TRY(od::launch_muon_scale(args, t, h->cfg.mu, nesterov, gbf, parts, h->cfg.eps, std::ldexp(1.0, h->first_exp), st));
     const NsArgs last = args;
@@ -420,11 +436,11 @@ static int muon_run(orthdion_muon_handle h, void* const* X, const void* const* G
       const Plan* plan = nullptr;
       args.count = 0;
       for (const Class& c : cl.classes)
-        if (s < c.plan->stages.size())
-          for (const PlannedJob& job : c.plan->stages[s])
+        if (s < c.plan[update]->stages.size())
+          for (const PlannedJob& job : c.plan[update]->stages[s])
             if (of(job.kind)) {
               add(c, job);
-              plan = c.plan;
+              plan = c.plan[update];
             }
       return plan;
     };
