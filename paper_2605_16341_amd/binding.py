@@ -3,6 +3,8 @@ convenience class.  Argument marshalling only - every step of the method runs in
 kernels.  There is no CPU fallback: a missing library is an error."""
 from __future__ import annotations
 
+import array
+import contextlib
 import ctypes
 import operator
 import os
@@ -230,7 +232,7 @@ def orthdion_set_variant(handle: int, variant: int) -> None:
 
 
 def _ptr_array(ptrs: Sequence[int]):
-    return (ctypes.c_void_p * len(ptrs))(*ptrs)
+    return (ctypes.c_void_p * len(ptrs)).from_buffer(array.array("Q", ptrs)) if ptrs else (ctypes.c_void_p * 0)()
 
 
 def orthdion_step(handle: int, X: Sequence[int], G: Sequence[int], M: Sequence[int], Q: Sequence[int],
@@ -514,6 +516,11 @@ def _dtypes(torch, x_dtype: str, g_dtype: Optional[str]):
 _dtype_of = operator.attrgetter("dtype")
 
 
+def _on_device(torch, index: int):
+    """A context in which device `index` is the current one."""
+    return contextlib.nullcontext() if torch.cuda.current_device() == index else torch.cuda.device(index)
+
+
 def _per_item(name: str, value, count: int) -> List[float]:
     """One float per item from one for all or a sequence."""
     got = [float(value)] * count if isinstance(value, (int, float)) else [float(v) for v in value]
@@ -585,13 +592,13 @@ class Muon:
         """One optimizer step: X and M are updated in place."""
         x, g = self._pointers("X", X, self._x_dtype, 0), self._pointers("G", G, self._g_dtype, 1)
         m = self._pointers("M", M, self._torch.float32, 2)
-        with self._torch.cuda.device(self.workspace.device):
+        with _on_device(self._torch, self.workspace.get_device()):
             orthdion_muon_step(self.handle, x, g, m, self.workspace.data_ptr(), self.workspace_bytes, self._stream(stream))
 
     def orthogonalise(self, A, out, stream=None) -> None:
         """The orthogonalised A (laid out as G) into `out` (laid out as X)."""
         a, o = self._pointers("A", A, self._g_dtype, 1), self._pointers("out", out, self._x_dtype, 0)
-        with self._torch.cuda.device(self.workspace.device):
+        with _on_device(self._torch, self.workspace.get_device()):
             orthdion_muon_orthogonalise(self.handle, a, o, self.workspace.data_ptr(), self.workspace_bytes, self._stream(stream))
 
     def info(self, stream=None) -> List[int]:
@@ -650,7 +657,7 @@ class AdamW:
                         raise ValueError(f"{name}[{i}]: need a contiguous {dtype} tensor of {self.lengths[i]} elements on {counter.device}, "
                                          f"got {t.dtype} {tuple(t.shape)} on {t.device}, contiguous={t.is_contiguous()}")
             addresses.append(list(map(tensor.data_ptr, seq)))
-        with torch.cuda.device(counter.device):
+        with _on_device(torch, counter.get_device()):
             orthdion_adamw_step(self.handle, *addresses, counter.data_ptr(),
                                 stream if stream is not None else torch.cuda.current_stream(counter.device).cuda_stream)
 

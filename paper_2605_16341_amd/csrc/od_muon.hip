@@ -232,10 +232,10 @@ __global__ __launch_bounds__(256) void k_muon_scale(NsArgs args, MuonTables t, f
 // ------------------------------------------------------------------------------------
 // The products.  One workgroup computes a T x T tile of C = A B over 64-deep steps; A has k along its rows, B is given
 // either as the rows of B^T with k along them (TRB = false) or as rows of B, k down its columns (TRB = true).  Both
-// operands come by direct-to-LDS loads into a ring of five operand tiles (A0 B0 A1 B1 A2 ..):
+// operands come by direct-to-LDS loads into a ring of operand tiles (A0 B0 A1 B1 ..):
 //   k along rows   128-byte rows, their 16-byte k-groups XOR-swizzled by (row >> 1) & 7: the 16 lanes that a
 //                  ds_read_b128 serves at a time lie in 16 different groups of four banks
-//   k down columns rows of T elements, their 64-byte blocks XOR-swizzled by k & 3, so that the four rows of a
+//   k down columns rows of T elements, their 64-byte blocks XOR-swizzled by k, so that the four rows of a
 //                  ds_read_b64_tr_b16 lie in different banks
 // With two parts a product is three passes over K: hi hi, hi lo, lo hi.
 // ------------------------------------------------------------------------------------
@@ -256,6 +256,10 @@ OD_DEV void static_for(F&& f) {
 }
 
 OD_DEV int swz64(int row) { return (row >> 1) & 7; }
+// the 16-byte slots by which row k of a tile with k down its columns is rotated: rows of 128 bytes lie in alternate halves
+// of the 256 bytes of all banks already
+template <int T>
+OD_DEV int swz_down(int k) { return T == 64 ? (k & 2) << 1 : (k & 3) << 2; }
 
 struct NsOperand {
   const uint16_t* p;      // tile's first row (TRB: the tile's first column is in `edge`)
@@ -264,13 +268,16 @@ struct NsOperand {
   int rows;               // rows (TRB: columns) from the tile's first one that may be read, at least 1 (TRB: 8)
 };
 
-template <int T_, int WI_, int WJ_>
+// D: steps that the loads run ahead, in a ring of 2 D + 1 operand tiles.  Two suffice where all CUs compute; a launch of few
+// workgroups, alone on their CUs, waits for memory and takes four (sums of 1024 products in three passes: 0.83 us a step at two).
+template <int T_, int WI_, int WJ_, int D_>
 struct NsTile {
-  static constexpr int T = T_, WI = WI_, WJ = WJ_, NW = WI * WJ, THREADS = 64 * NW;
+  static constexpr int T = T_, WI = WI_, WJ = WJ_, NW = WI * WJ, THREADS = 64 * NW, D = D_;
   static constexpr int WTM = T / WI, WTN = T / WJ, FM = WTM / 32, FN = WTN / 32;
-  static constexpr int OPER = T * 128, RING = 5, LDS = RING * OPER;          // bytes of a tile's operand step, ring
-  static constexpr int BLOCKS = T == 128 ? 2 : 1;                             // workgroups per CU
+  static constexpr int OPER = T * 128, RING = 2 * D + 1, LDS = RING * OPER;  // bytes of a tile's operand step, ring
+  static constexpr int BLOCKS = LDS <= 81920 ? 2 : 1;                         // workgroups per CU
   static constexpr int CH = T / 8 / NW;                                       // 1 KB loads per wave and operand tile
+  static_assert((2 * D - 2) * CH < 64, "loads in flight that vmcnt can count");
 };
 
 // ACROSS: the accumulator of lane l holds C[l % 32][4 consecutive columns], otherwise C[4 consecutive rows][l % 32]
@@ -289,7 +296,7 @@ OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const 
     va[j] = (uint32_t)min(row, A.rows - 1) * (uint32_t)(A.ld * 2) + kg * 16;
     if constexpr (TRB) {
       constexpr int SLOTS = T / 8;                       // 16-byte groups of a row
-      const int k = chunk * (64 / SLOTS) + lane / SLOTS, cg = (lane % SLOTS) ^ ((k & 3) << 2);
+      const int k = chunk * (64 / SLOTS) + lane / SLOTS, cg = (lane % SLOTS) ^ swz_down<T>(k);
       vb[j] = (uint32_t)k * (uint32_t)(B.ld * 2) + min(cg * 8, B.rows - 8) * 2;
     } else {
       vb[j] = (uint32_t)min(row, B.rows - 1) * (uint32_t)(B.ld * 2) + kg * 16;
@@ -338,7 +345,7 @@ OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const 
       if constexpr (TRB) {
         const int k = sub * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2);
         const int col = wj * TL::WTN + 32 * j + ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
-        const int at = k * (2 * T) + (((col >> 3) ^ ((k & 3) << 2)) << 4) + (col & 7) * 2;
+        const int at = k * (2 * T) + (((col >> 3) ^ swz_down<T>(k)) << 4) + (col & 7) * 2;
         typedef __attribute__((address_space(3))) s16x4* lptr;
         const char* p = at_b + at;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(p));
@@ -376,22 +383,23 @@ OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const 
 
   // Step i multiplies quarters 0 .. 3 of A(i), B(i), each from registers that were read during the quarter before.  The last
   // quarter comes behind the barrier that frees the tiles of step i and admits those of step i + 1, so no product
-  // waits for the first operands of a step.  B(i + 2) is loaded right behind that barrier, A(i + 3) during the following
-  // three quarters: the loads are spread over the step, and the ones issued late have a step more to arrive.
+  // waits for the first operands of a step.  B(i + D) is loaded right behind that barrier, A(i + D + 1) during the following
+  // three quarters: the loads are spread over the step.
   constexpr int C0 = (CH + 1) / 2, C1 = (CH - C0 + 1) / 2, C2 = CH - C0 - C1;
-  static_for<4>([&](auto u) {
+  constexpr int D = TL::D;
+  static_for<2 * D>([&](auto u) {
     const Loads l = loads_of(decltype(u)::value / 2, decltype(u)::value % 2);
     static_for<CH>([&](auto j) {
       if constexpr (decltype(u)::value % 2) issue_b(l, j);
       else issue_a(l, j);
     });
   });
-  __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * CH));
+  __builtin_amdgcn_s_waitcnt(vmcnt_only((2 * D - 2) * CH));
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   fetch(0, 0, even);
   for (int i = 0; i < steps; ++i) {
-    const Loads la = loads_of(i + 2, false), lb = loads_of(i + 2, true);
+    const Loads la = loads_of(i + D, false), lb = loads_of(i + D, true);
     auto from_a = [&](auto j) { issue_a(la, j); };
     fetch(i, 1, odd);
     __builtin_amdgcn_sched_barrier(0);
@@ -402,8 +410,8 @@ OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const 
     fetch(i, 3, odd);
     __builtin_amdgcn_sched_barrier(0);
     products(even, std::integral_constant<int, C0 + C1>{}, std::integral_constant<int, C2>{}, from_a);
-    // this wave's reads of step i are done, and all its loads but those of A(i + 2)
-    __builtin_amdgcn_s_waitcnt(vmcnt_only(CH));
+    // this wave's reads of step i are done, and its loads up to B(i + 1): A(i + 2) .. A(i + D) may be under way
+    __builtin_amdgcn_s_waitcnt(vmcnt_only((2 * D - 3) * CH));
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -771,48 +779,60 @@ __global__ __launch_bounds__(TL::THREADS, TL::BLOCKS) void k_ns_final(NsArgs arg
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i0 = ti * T + wave / TL::WJ * TL::WTM, j0 = tj * T + wave % TL::WJ * TL::WTN;
-  const bool vec = (reinterpret_cast<uintptr_t>(e.X) & (XBF ? 7 : 15)) == 0 && (a.ldx & 3) == 0;
+  const bool vec = rows_aligned(e.X, a.ldx);
   const float step = update ? lr * a.scale * scale : -scale;
   const float kx = update ? keep : 0.f;
-  // accumulators one by one: the four runs of a lane are loaded together, then written
-  static_for<TL::FM * TL::FN>([&](auto n) {
-    constexpr int i = decltype(n)::value / TL::FN, j = decltype(n)::value % TL::FN;
-    const int row = TALL ? j0 + 32 * j + (lane & 31) : i0 + 32 * i + (lane & 31);
-    const int col = (TALL ? i0 + 32 * i : j0 + 32 * j) + 4 * (lane >> 5);
-    if (row >= a.m) return;
-    const int64_t at = (int64_t)row * a.ldx + col;
-    float x[4][4];
+  // 32 rows of the matrix at a time through the wave's own part of LDS, from where a lane takes eight columns of a row
+  constexpr int COLS = TALL ? TL::WTM : TL::WTN, PITCH = COLS * 4 + 16, GROUPS = COLS / 8;
+  static_assert(TL::NW * 32 * PITCH <= TL::LDS, "staging");
+  char* mine = lds + wave * (32 * PITCH);
+  __syncthreads();
+  static_for<TALL ? TL::FN : TL::FM>([&](auto bb) {
+    constexpr int blk = decltype(bb)::value;
+    static_for<COLS / 32 * 4>([&](auto n) {
+      constexpr int c = decltype(n)::value / 4, v4 = decltype(n)::value % 4;
+      const f32x16& v = acc[TALL ? c : blk][TALL ? blk : c];
+      *reinterpret_cast<f32x4*>(mine + (lane & 31) * PITCH + (32 * c + 8 * v4 + 4 * (lane >> 5)) * 4) = f32x4{v[4 * v4], v[4 * v4 + 1], v[4 * v4 + 2], v[4 * v4 + 3]};
+    });
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int v4 = 0; v4 < 4; ++v4) {
+    for (int it = 0; it < GROUPS / 2; ++it) {
+      const int k = it * 64 + lane, r = k / GROUPS, g = k % GROUPS;
+      const int row = (TALL ? j0 : i0) + 32 * blk + r, col = (TALL ? i0 : j0) + 8 * g;
+      if (row >= a.m || col >= a.n) continue;
+      const f32x4* o = reinterpret_cast<const f32x4*>(mine + r * PITCH + g * 32);
+      const f32x4 o0 = o[0], o1 = o[1];
+      const int64_t at = (int64_t)row * a.ldx + col;
+      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      const bool whole = vec && col + 8 <= a.n;
+      if (update) {
+        if (whole) load8<XBF>(e.X, at, x);
+        else {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) x[v4][k] = 0.f;
-      if (!update || col + 8 * v4 >= a.n) continue;
-      if (vec && col + 8 * v4 + 4 <= a.n) {
-        if constexpr (XBF) SrcBF16::unpack4(*reinterpret_cast<const u32x2*>(reinterpret_cast<const uint16_t*>(e.X) + at + 8 * v4), x[v4]);
-        else SrcF32::unpack4(*reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(e.X) + at + 8 * v4), x[v4]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (col + 8 * v4 + k < a.n) x[v4][k] = load_elem<XBF>(e.X, at + 8 * v4 + k);
+          for (int q = 0; q < 8; ++q)
+            if (col + q < a.n) x[q] = load_elem<XBF>(e.X, at + q);
+        }
       }
-    }
 #pragma unroll
-    for (int v4 = 0; v4 < 4; ++v4) {
-      if (col + 8 * v4 >= a.n) continue;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[v4][k] = kx * x[v4][k] - step * acc[i][j][4 * v4 + k];
-      if (vec && col + 8 * v4 + 4 <= a.n) {
-        if constexpr (XBF) *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(e.X) + at + 8 * v4) = u32x2{pack_bf16_rne(x[v4][0], x[v4][1]), pack_bf16_rne(x[v4][2], x[v4][3])};
-        else *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(e.X) + at + 8 * v4) = f32x4{x[v4][0], x[v4][1], x[v4][2], x[v4][3]};
+      for (int q = 0; q < 8; ++q) x[q] = kx * x[q] - step * (q < 4 ? o0[q & 3] : o1[q & 3]);
+      if (whole) {
+        if constexpr (XBF) {
+          *reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(e.X) + at) = u32x4{pack_bf16_rne(x[0], x[1]), pack_bf16_rne(x[2], x[3]), pack_bf16_rne(x[4], x[5]), pack_bf16_rne(x[6], x[7])};
+        } else {
+          f32x4* px = reinterpret_cast<f32x4*>(reinterpret_cast<float*>(e.X) + at);
+          px[0] = f32x4{x[0], x[1], x[2], x[3]};
+          px[1] = f32x4{x[4], x[5], x[6], x[7]};
+        }
       } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (col + 8 * v4 + k >= a.n) continue;
-          if constexpr (XBF) reinterpret_cast<uint16_t*>(e.X)[at + 8 * v4 + k] = (uint16_t)pack_bf16_rne(x[v4][k], 0.f);
-          else reinterpret_cast<float*>(e.X)[at + 8 * v4 + k] = x[v4][k];
+        for (int q = 0; q < 8; ++q) {
+          if (col + q >= a.n) continue;
+          if constexpr (XBF) reinterpret_cast<uint16_t*>(e.X)[at + q] = (uint16_t)pack_bf16_rne(x[q], 0.f);
+          else reinterpret_cast<float*>(e.X)[at + q] = x[q];
         }
       }
     }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   });
 }
 
@@ -873,12 +893,11 @@ hipError_t go(K* kernel, const NsJobs<N>& a, hipStream_t st, A... rest) {
   return hipGetLastError();
 }
 
-typedef NsTile<128, 2, 2> Small;
-#ifdef TRY
-typedef TRY Large;
-#else
-typedef NsTile<256, 2, 4> Large;
-#endif
+typedef NsTile<64, 2, 2, 4> Tiny;
+typedef NsTile<128, 2, 2, 4> Deep;
+typedef NsTile<128, 2, 2, 2> Small;
+typedef NsTile<256, 2, 4, 2> Large;
+static_assert(Deep::T == kNsSplitTile, "partial sums are those of its tiles");
 
 template <int T>
 int tiles_of(const NsJob& c) {
@@ -889,13 +908,26 @@ int tiles_of(const NsJob& c) {
 #ifndef WIDE
 #define WIDE 160
 #endif
-bool large(const NsArgs& a) {
-  int64_t n = 0;
+#ifndef DEEP
+#define DEEP 256
+#endif
+#ifndef TINY
+#define TINY 64
+#endif
+// f with the tile for these jobs
+template <class F>
+hipError_t with_tile(const NsArgs& a, F&& f) {
+  int64_t n128 = 0, n256 = 0;
+  bool partial = false;
   for (int k = 0; k < a.count; ++k) {
-    if (a.j[k].splits > 0) return false;     // partial sums are those of tiles of kNsSplitTile
-    n += (int64_t)a.j[k].nb * tiles_of<256>(a.j[k]);
+    partial = partial || a.j[k].splits > 0;
+    n128 += (int64_t)a.j[k].nb * tiles_of<128>(a.j[k]);
+    n256 += (int64_t)a.j[k].nb * tiles_of<256>(a.j[k]);
   }
-  return n >= WIDE;
+  if (partial) return n128 <= DEEP ? f(Deep{}) : f(Small{});
+  if (n256 >= WIDE) return f(Large{});
+  if (n128 < TINY) return f(Tiny{});
+  return n128 <= DEEP ? f(Deep{}) : f(Small{});
 }
 
 template <class TL, int PARTS, bool XBF>
@@ -929,7 +961,7 @@ hipError_t launch_muon_scale(const NsArgs& a, const MuonTables& t, float mu, boo
 }
 
 hipError_t launch_ns_products(const NsArgs& a, int parts, hipStream_t st) {
-  return large(a) ? products_of<Large>(a, parts, st) : products_of<Small>(a, parts, st);
+  return with_tile(a, [&](auto tile) { return products_of<decltype(tile)>(a, parts, st); });
 }
 
 hipError_t launch_ns_reduce(const NsArgs& a, int parts, hipStream_t st) {
@@ -956,7 +988,7 @@ hipError_t launch_ns_small(const NsArgs& a, const NsSteps& steps, int parts, hip
 }
 
 hipError_t launch_ns_final(const NsArgs& a, const MuonTables& t, int parts, bool update, float keep, float lr, bool x_bf16, hipStream_t st) {
-  return large(a) ? final_tiles<Large>(a, t, parts, update, keep, lr, x_bf16, st) : final_tiles<Small>(a, t, parts, update, keep, lr, x_bf16, st);
+  return with_tile(a, [&](auto tile) { return final_tiles<decltype(tile)>(a, t, parts, update, keep, lr, x_bf16, st); });
 }
 
 }  // namespace od
