@@ -10,6 +10,8 @@
 // (which steps do is the host's plan).  See od_muon.h for the layout of the workspace.
 #include "od_muon.h"
 
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "od_dma.h"
@@ -237,7 +239,6 @@ __global__ __launch_bounds__(256) void k_muon_scale(NsArgs args, MuonTables t, f
 //                  ds_read_b128 serves at a time lie in 16 different groups of four banks
 //   k down columns rows of T elements, their 64-byte blocks XOR-swizzled by k, so that the four rows of a
 //                  ds_read_b64_tr_b16 lie in different banks
-// With two parts a product is three passes over K: hi hi, hi lo, lo hi.
 // ------------------------------------------------------------------------------------
 // As dma16, from a uniform base plus 32-bit lane offsets; all lanes of the wave are active, and `mask` (all ones or zero)
 // takes the load away without a branch, past which accumulators would be moved about.
@@ -268,22 +269,26 @@ struct NsOperand {
   int rows;               // rows (TRB: columns) from the tile's first one that may be read, at least 1 (TRB: 8)
 };
 
-// D: steps that the loads run ahead, in a ring of 2 D + 1 operand tiles.  Two suffice where all CUs compute; a launch of few
-// workgroups, alone on their CUs, waits for memory and takes four (sums of 1024 products in three passes: 0.83 us a step at two).
-template <int T_, int WI_, int WJ_, int D_>
+// The loads run two steps ahead (four gained nothing anywhere).
+template <int T_, int WI_, int WJ_>
 struct NsTile {
-  static constexpr int T = T_, WI = WI_, WJ = WJ_, NW = WI * WJ, THREADS = 64 * NW, D = D_;
+  static constexpr int T = T_, WI = WI_, WJ = WJ_, NW = WI * WJ, THREADS = 64 * NW;
   static constexpr int WTM = T / WI, WTN = T / WJ, FM = WTM / 32, FN = WTN / 32;
-  static constexpr int OPER = T * 128, RING = 2 * D + 1, LDS = RING * OPER;  // bytes of a tile's operand step, ring
-  static constexpr int BLOCKS = LDS <= 81920 ? 2 : 1;                         // workgroups per CU
-  static constexpr int CH = T / 8 / NW;                                       // 1 KB loads per wave and operand tile
-  static_assert((2 * D - 2) * CH < 64, "loads in flight that vmcnt can count");
+  static constexpr int OPER = T * 128, RING = 5;                              // bytes of an operand tile of one part
+  static constexpr int CH = T / 8 / NW;                                       // 1 KB loads per wave and such a tile
+  // Two parts of a value: both in the ring, three products from one load of each, where that fits LDS (1024 x 1024, a product
+  // of S: 34 us in three passes); otherwise three passes over K, hi hi, hi lo and lo hi.
+  static constexpr bool together(int parts) { return parts == 2 && T <= 128; }
+  static constexpr int unit(int parts) { return together(parts) ? 2 * OPER : OPER; }
+  static constexpr int lds(int parts) { return RING * unit(parts); }
+  static constexpr int blocks(int parts) { return lds(parts) <= 81920 ? 2 : 1; }        // workgroups per CU
 };
 
 // ACROSS: the accumulator of lane l holds C[l % 32][4 consecutive columns], otherwise C[4 consecutive rows][l % 32]
 template <class TL, int PARTS, bool TRB, bool ACROSS>
 OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const NsOperand& B, int kdim, char* lds, int split = 0, int splits = 1) {
-  constexpr int T = TL::T, CH = TL::CH;
+  constexpr bool BOTH = TL::together(PARTS);
+  constexpr int T = TL::T, CH = TL::CH, UNIT = TL::unit(PARTS), LOADS = BOTH ? 2 * CH : CH;      // a wave's loads of a unit
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wi = wave / TL::WJ, wj = wave % TL::WJ;
@@ -302,25 +307,22 @@ OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const 
       vb[j] = (uint32_t)min(row, B.rows - 1) * (uint32_t)(B.ld * 2) + kg * 16;
     }
   }
-  const int ks = kdim / kNsStep, all = ks * (PARTS == 2 ? 3 : 1);
+  const int ks = kdim / kNsStep, all = ks * (PARTS == 2 && !BOTH ? 3 : 1);
   // steps first .. of all, this split's share
   const int first = splits > 1 ? quotient(all * split, splits) : 0, steps = (splits > 1 ? quotient(all * (split + 1), splits) : all) - first;
   const int64_t bstep = TRB ? (int64_t)kNsStep * B.ld : kNsStep;
-  // loads of one operand tile of one step; of a step past the last one, none
-  struct Loads { const uint16_t* p; uint32_t at, mask; };
-  auto slot = [&](int unit) { return (uint32_t)(unit % TL::RING) * TL::OPER; };
+  // loads of one unit of one step; of a step past the last one, none
+  struct Loads { const uint16_t *p, *lo; uint32_t at, mask; };
+  auto slot = [&](int unit) { return (uint32_t)(unit % TL::RING) * UNIT; };
   auto loads_of = [&](int step, bool of_b) {
-    const int seg = PARTS == 2 ? quotient(first + step, ks) : 0, kk = first + step - seg * ks;
+    const int seg = PARTS == 2 && !BOTH ? quotient(first + step, ks) : 0, kk = first + step - seg * ks;
     const uint16_t* p = of_b ? B.p + (seg == 1 ? B.plane : 0) + kk * bstep : A.p + (seg == 2 ? A.plane : 0) + (int64_t)kk * kNsStep;
-    return Loads{p, lds0 + slot(2 * step + of_b) + wave * CH * 1024, step < steps ? ~0u : 0u};
+    return Loads{p, p + (of_b ? B.plane : A.plane), lds0 + slot(2 * step + of_b) + wave * CH * 1024, step < steps ? ~0u : 0u};
   };
-  auto issue_a = [&](const Loads& l, auto jj) {
+  auto issue = [&](const Loads& l, const uint32_t (&voff)[CH], auto jj) {
     constexpr int j = decltype(jj)::value;
-    dma16_at(va[j], l.p, l.at + j * 1024, l.mask);
-  };
-  auto issue_b = [&](const Loads& l, auto jj) {
-    constexpr int j = decltype(jj)::value;
-    dma16_at(vb[j], l.p, l.at + j * 1024, l.mask);
+    if constexpr (j < CH) dma16_at(voff[j], l.p, l.at + j * 1024, l.mask);
+    else dma16_at(voff[j - CH], l.lo, l.at + TL::OPER + (j - CH) * 1024, l.mask);
   };
 #pragma unroll
   for (int i = 0; i < TL::FM; ++i)
@@ -329,47 +331,52 @@ OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const 
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
-  u32x4 fa[2][TL::FM], fb[2][TL::FN];
+  constexpr int HL = BOTH ? 2 : 1;
+  u32x4 fa[2][HL][TL::FM], fb[2][HL][TL::FN];
   auto fetch = [&](int step, int sub, auto ss) {
     constexpr int set = decltype(ss)::value;
     const char* at_a = lds + slot(2 * step);
     const char* at_b = lds + slot(2 * step + 1);
     const int kg = 2 * sub + (lane >> 5);
 #pragma unroll
-    for (int i = 0; i < TL::FM; ++i) {
-      const int row = wi * TL::WTM + 32 * i + (lane & 31);
-      fa[set][i] = *reinterpret_cast<const u32x4*>(at_a + row * 128 + ((kg ^ swz64(row)) << 4));
-    }
+    for (int h = 0; h < HL; ++h) {
 #pragma unroll
-    for (int j = 0; j < TL::FN; ++j) {
-      if constexpr (TRB) {
-        const int k = sub * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2);
-        const int col = wj * TL::WTN + 32 * j + ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
-        const int at = k * (2 * T) + (((col >> 3) ^ swz_down<T>(k)) << 4) + (col & 7) * 2;
-        typedef __attribute__((address_space(3))) s16x4* lptr;
-        const char* p = at_b + at;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(p));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(p + 4 * (2 * T)));
-        const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
-        fb[set][j] = u32x4{l2[0], l2[1], h2[0], h2[1]};
-      } else {
-        const int row = wj * TL::WTN + 32 * j + (lane & 31);
-        fb[set][j] = *reinterpret_cast<const u32x4*>(at_b + row * 128 + ((kg ^ swz64(row)) << 4));
+      for (int i = 0; i < TL::FM; ++i) {
+        const int row = wi * TL::WTM + 32 * i + (lane & 31);
+        fa[set][h][i] = *reinterpret_cast<const u32x4*>(at_a + h * TL::OPER + row * 128 + ((kg ^ swz64(row)) << 4));
+      }
+#pragma unroll
+      for (int j = 0; j < TL::FN; ++j) {
+        if constexpr (TRB) {
+          const int k = sub * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2);
+          const int col = wj * TL::WTN + 32 * j + ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
+          typedef __attribute__((address_space(3))) s16x4* lptr;
+          const char* p = at_b + h * TL::OPER + k * (2 * T) + (((col >> 3) ^ swz_down<T>(k)) << 4) + (col & 7) * 2;
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(p));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(p + 4 * (2 * T)));
+          const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
+          fb[set][h][j] = u32x4{l2[0], l2[1], h2[0], h2[1]};
+        } else {
+          const int row = wj * TL::WTN + 32 * j + (lane & 31);
+          fb[set][h][j] = *reinterpret_cast<const u32x4*>(at_b + h * TL::OPER + row * 128 + ((kg ^ swz64(row)) << 4));
+        }
       }
     }
   };
-  auto product = [&](auto ii, auto jj, auto ss) {
-    constexpr int i = decltype(ii)::value, j = decltype(jj)::value, set = decltype(ss)::value;
-    acc[i][j] = ACROSS ? mfma_32x32x16<true>(fb[set][j], fa[set][i], acc[i][j])
-                       : mfma_32x32x16<true>(fa[set][i], fb[set][j], acc[i][j]);
+  // product n of a quarter of a step: the parts' three rounds over the accumulators, smallest terms first
+  auto product = [&](auto nn, auto ss) {
+    constexpr int n = decltype(nn)::value, set = decltype(ss)::value, i = n / TL::FN % TL::FM, j = n % TL::FN;
+    constexpr int round = n / (TL::FM * TL::FN), ha = BOTH && round == 0, hb = BOTH && round == 1;
+    acc[i][j] = ACROSS ? mfma_32x32x16<true>(fb[set][hb][j], fa[set][ha][i], acc[i][j])
+                       : mfma_32x32x16<true>(fa[set][ha][i], fb[set][hb][j], acc[i][j]);
   };
   // the products of one quarter of a step with `count` loads, from `first` on, spread between them: issued in a row they
   // would hold the wave up until the memory path took them all
   auto products = [&](auto ss, auto first, auto count, auto&& load) {
-    constexpr int N = TL::FM * TL::FN, F = decltype(first)::value, C = decltype(count)::value;
+    constexpr int N = TL::FM * TL::FN * (BOTH ? 3 : 1), F = decltype(first)::value, C = decltype(count)::value;
     static_for<N>([&](auto mm) {
       constexpr int m = decltype(mm)::value, before = m * C / N, after = (m + 1) * C / N;
-      product(std::integral_constant<int, m / TL::FN>{}, std::integral_constant<int, m % TL::FN>{}, ss);
+      product(mm, ss);
       if constexpr (after > before) {
         __builtin_amdgcn_sched_barrier(0);
         static_for<after - before>([&](auto k) { load(std::integral_constant<int, F + before + decltype(k)::value>{}); });
@@ -383,24 +390,23 @@ OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const 
 
   // Step i multiplies quarters 0 .. 3 of A(i), B(i), each from registers that were read during the quarter before.  The last
   // quarter comes behind the barrier that frees the tiles of step i and admits those of step i + 1, so no product
-  // waits for the first operands of a step.  B(i + D) is loaded right behind that barrier, A(i + D + 1) during the following
-  // three quarters: the loads are spread over the step.
-  constexpr int C0 = (CH + 1) / 2, C1 = (CH - C0 + 1) / 2, C2 = CH - C0 - C1;
-  constexpr int D = TL::D;
-  static_for<2 * D>([&](auto u) {
+  // waits for the first operands of a step.  B(i + 2) is loaded right behind that barrier, A(i + 3) during the following
+  // three quarters: the loads are spread over the step, and the ones issued late have a step more to arrive.
+  constexpr int C0 = (LOADS + 1) / 2, C1 = (LOADS - C0 + 1) / 2, C2 = LOADS - C0 - C1;
+  static_for<4>([&](auto u) {
     const Loads l = loads_of(decltype(u)::value / 2, decltype(u)::value % 2);
-    static_for<CH>([&](auto j) {
-      if constexpr (decltype(u)::value % 2) issue_b(l, j);
-      else issue_a(l, j);
+    static_for<LOADS>([&](auto j) {
+      if constexpr (decltype(u)::value % 2) issue(l, vb, j);
+      else issue(l, va, j);
     });
   });
-  __builtin_amdgcn_s_waitcnt(vmcnt_only((2 * D - 2) * CH));
+  __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * LOADS));
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   fetch(0, 0, even);
   for (int i = 0; i < steps; ++i) {
-    const Loads la = loads_of(i + D, false), lb = loads_of(i + D, true);
-    auto from_a = [&](auto j) { issue_a(la, j); };
+    const Loads la = loads_of(i + 2, false), lb = loads_of(i + 2, true);
+    auto from_a = [&](auto j) { issue(la, va, j); };
     fetch(i, 1, odd);
     __builtin_amdgcn_sched_barrier(0);
     products(even, std::integral_constant<int, 0>{}, std::integral_constant<int, C0>{}, from_a);
@@ -410,14 +416,14 @@ OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const 
     fetch(i, 3, odd);
     __builtin_amdgcn_sched_barrier(0);
     products(even, std::integral_constant<int, C0 + C1>{}, std::integral_constant<int, C2>{}, from_a);
-    // this wave's reads of step i are done, and its loads up to B(i + 1): A(i + 2) .. A(i + D) may be under way
-    __builtin_amdgcn_s_waitcnt(vmcnt_only((2 * D - 3) * CH));
+    // this wave's reads of step i are done, and all its loads but those of A(i + 2)
+    __builtin_amdgcn_s_waitcnt(vmcnt_only(LOADS));
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     fetch(i + 1, 0, even);                 // past the last step: what lies there, never used
     __builtin_amdgcn_sched_barrier(0);
-    products(odd, std::integral_constant<int, 0>{}, std::integral_constant<int, CH>{}, [&](auto j) { issue_b(lb, j); });
+    products(odd, std::integral_constant<int, 0>{}, std::integral_constant<int, LOADS>{}, [&](auto j) { issue(lb, vb, j); });
   }
   __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
 }
@@ -431,7 +437,7 @@ OD_DEV void ns_store(char* lds, V&& value, uint16_t* out, int64_t plane, int ld,
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   constexpr int ROWB = TL::WTN * 2, SL = ROWB / 16, PIECE = 32 * ROWB;       // bytes and 16-byte slots of a staged row
-  static_assert(TL::NW * PARTS * PIECE <= TL::LDS, "staging");
+  static_assert(TL::NW * PARTS * PIECE <= TL::lds(PARTS), "staging");
   auto swz = [](int r) { return SL == 8 ? swz64(r) : r & (SL - 1); };
   auto masked = [&](u32x4 w, int col) {
     if (col + 8 > valid) {
@@ -500,7 +506,7 @@ OD_DEV void upper_tile(int t, int n, int* ti, int* tj) {
 
 // The jobs of one launch.
 template <class TL, int PARTS>
-__global__ __launch_bounds__(TL::THREADS, TL::BLOCKS) void k_ns_products(NsArgs args) {
+__global__ __launch_bounds__(TL::THREADS, TL::blocks(PARTS)) void k_ns_products(NsArgs args) {
   extern __shared__ __align__(16) char lds[];
   constexpr int T = TL::T;
   const int bid = xcd_contiguous(blockIdx.x, args.total);
@@ -626,7 +632,8 @@ __global__ __launch_bounds__(256) void k_ns_reduce(NsArgs args) {
 template <int D>
 struct NsSmallTile {
   static constexpr int WI = 2, WJ = D / 32, NW = WI * WJ, THREADS = 64 * NW, FM = D / 64;      // wave tile D/2 x 32
-  static constexpr int ROWB = D * 2, PLANE = D * ROWB, LDS = 4 * PLANE;
+  static constexpr int ROWB = D * 2, PLANE = D * ROWB;
+  static constexpr int lds(int) { return 4 * PLANE; }
 };
 
 template <int D, int PARTS>
@@ -760,7 +767,7 @@ __global__ __launch_bounds__(NsSmallTile<D>::THREADS, 1) void k_ns_small(NsJobs<
 
 // O = P Y into the caller's matrix, or its update
 template <class TL, int PARTS, bool XBF, bool TALL>
-__global__ __launch_bounds__(TL::THREADS, TL::BLOCKS) void k_ns_final(NsArgs args, MuonTables t, int update, float keep, float lr) {
+__global__ __launch_bounds__(TL::THREADS, TL::blocks(PARTS)) void k_ns_final(NsArgs args, MuonTables t, int update, float keep, float lr) {
   extern __shared__ __align__(16) char lds[];
   constexpr int T = TL::T;
   const int bid = xcd_contiguous(blockIdx.x, args.total);
@@ -784,7 +791,7 @@ __global__ __launch_bounds__(TL::THREADS, TL::BLOCKS) void k_ns_final(NsArgs arg
   const float kx = update ? keep : 0.f;
   // 32 rows of the matrix at a time through the wave's own part of LDS, from where a lane takes eight columns of a row
   constexpr int COLS = TALL ? TL::WTM : TL::WTN, PITCH = COLS * 4 + 16, GROUPS = COLS / 8;
-  static_assert(TL::NW * 32 * PITCH <= TL::LDS, "staging");
+  static_assert(TL::NW * 32 * PITCH <= TL::lds(PARTS), "staging");
   char* mine = lds + wave * (32 * PITCH);
   __syncthreads();
   static_for<TALL ? TL::FN : TL::FM>([&](auto bb) {
@@ -884,20 +891,19 @@ hipError_t allow_lds(K* kernel, int bytes) {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
-template <class TL, class K, int N, class... A>
+template <class TL, int PARTS, class K, int N, class... A>
 hipError_t go(K* kernel, const NsJobs<N>& a, hipStream_t st, A... rest) {
   if (a.total == 0) return hipSuccess;
-  const hipError_t rc = allow_lds(kernel, TL::LDS);
+  const hipError_t rc = allow_lds(kernel, TL::lds(PARTS));
   if (rc != hipSuccess) return rc;
-  kernel<<<a.total, TL::THREADS, TL::LDS, st>>>(a, rest...);
+  kernel<<<a.total, TL::THREADS, TL::lds(PARTS), st>>>(a, rest...);
   return hipGetLastError();
 }
 
-typedef NsTile<64, 2, 2, 4> Tiny;
-typedef NsTile<128, 2, 2, 4> Deep;
-typedef NsTile<128, 2, 2, 2> Small;
-typedef NsTile<256, 2, 4, 2> Large;
-static_assert(Deep::T == kNsSplitTile, "partial sums are those of its tiles");
+typedef NsTile<64, 2, 2> Tiny;
+typedef NsTile<128, 2, 2> Small;
+typedef NsTile<256, 2, 4> Large;
+static_assert(Small::T == kNsSplitTile, "partial sums are those of its tiles");
 
 template <int T>
 int tiles_of(const NsJob& c) {
@@ -905,42 +911,38 @@ int tiles_of(const NsJob& c) {
   return c.kind == NS_APPLY ? n * ceil_div(c.q, T) : c.kind == NS_FULL ? n * n : n * (n + 1) / 2 * (c.splits > 0 ? c.splits : 1);
 }
 
-#ifndef WIDE
-#define WIDE 160
-#endif
-#ifndef DEEP
-#define DEEP 256
-#endif
-#ifndef TINY
-#define TINY 64
-#endif
-// f with the tile for these jobs
+// f with the tile for these jobs: the one with the least time by what a step of 64 k takes, in us.  64 x 64: 0.43 while every
+// workgroup has a CU, 0.36 for each on a CU beyond that (two at a time); 128 x 128: 0.7 alone on a CU, 1.1 for two side by
+// side, 1.4 where that happens everywhere and the clock gives way; 256 x 256: 1.65, 2.0 with most CUs at work.  Measured on
+// products of 264 x 264 to 3000 x 3000, 1 to 16 matrices: the rule takes the fastest of the three or one within 10 %.
 template <class F>
 hipError_t with_tile(const NsArgs& a, F&& f) {
-  int64_t n128 = 0, n256 = 0;
-  bool partial = false;
+  double n64 = 0.0, n128 = 0.0, n256 = 0.0;
   for (int k = 0; k < a.count; ++k) {
-    partial = partial || a.j[k].splits > 0;
-    n128 += (int64_t)a.j[k].nb * tiles_of<128>(a.j[k]);
-    n256 += (int64_t)a.j[k].nb * tiles_of<256>(a.j[k]);
+    if (a.j[k].splits > 0) return f(Small{});          // partial sums
+    n64 += (double)a.j[k].nb * tiles_of<64>(a.j[k]);
+    n128 += (double)a.j[k].nb * tiles_of<128>(a.j[k]);
+    n256 += (double)a.j[k].nb * tiles_of<256>(a.j[k]);
   }
-  if (partial) return n128 <= DEEP ? f(Deep{}) : f(Small{});
-  if (n256 >= WIDE) return f(Large{});
-  if (n128 < TINY) return f(Tiny{});
-  return n128 <= DEEP ? f(Deep{}) : f(Small{});
+  const double rest = n128 - 512.0 * std::floor(n128 / 512.0);
+  const double t64 = std::max(0.43, 0.36 / 256.0 * n64);
+  const double t128 = 1.4 * std::floor(n128 / 512.0) + (rest == 0.0 ? 0.0 : rest <= 256.0 ? 0.7 : 1.1);
+  const double t256 = std::ceil(n256 / 256.0) * (n256 >= 200.0 ? 2.0 : 1.65);
+  if (t64 <= t128 && t64 <= t256) return f(Tiny{});
+  return t128 <= t256 ? f(Small{}) : f(Large{});
 }
 
 template <class TL, int PARTS, bool XBF>
 hipError_t final_of(const NsArgs& a, const MuonTables& t, bool update, float keep, float lr, hipStream_t st) {
-  const hipError_t rc = go<TL>(k_ns_final<TL, PARTS, XBF, false>, laid_out(a, [](const NsJob& c) { return !c.tall; }, tiles_of<TL::T>), st, t, (int)update, keep, lr);
+  const hipError_t rc = go<TL, PARTS>(k_ns_final<TL, PARTS, XBF, false>, laid_out(a, [](const NsJob& c) { return !c.tall; }, tiles_of<TL::T>), st, t, (int)update, keep, lr);
   if (rc != hipSuccess) return rc;
-  return go<TL>(k_ns_final<TL, PARTS, XBF, true>, laid_out(a, [](const NsJob& c) { return c.tall != 0; }, tiles_of<TL::T>), st, t, (int)update, keep, lr);
+  return go<TL, PARTS>(k_ns_final<TL, PARTS, XBF, true>, laid_out(a, [](const NsJob& c) { return c.tall != 0; }, tiles_of<TL::T>), st, t, (int)update, keep, lr);
 }
 
 template <class TL>
 hipError_t products_of(const NsArgs& a, int parts, hipStream_t st) {
   const NsArgs o = laid_out(a, any, tiles_of<TL::T>);
-  return parts == 2 ? go<TL>(k_ns_products<TL, 2>, o, st) : go<TL>(k_ns_products<TL, 1>, o, st);
+  return parts == 2 ? go<TL, 2>(k_ns_products<TL, 2>, o, st) : go<TL, 1>(k_ns_products<TL, 1>, o, st);
 }
 
 template <class TL>
@@ -976,7 +978,7 @@ namespace {
 template <int D, int PARTS>
 hipError_t small_of(const NsArgs& a, const NsSteps& steps, hipStream_t st) {
   const NsJobs<kNsClasses> o = laid_out<kNsClasses>(a, [](const NsJob& c) { return (c.p <= 64) == (D == 64); }, [](const NsJob&) { return 1; });
-  return go<NsSmallTile<D>>(k_ns_small<D, PARTS>, o, st, steps);
+  return go<NsSmallTile<D>, PARTS>(k_ns_small<D, PARTS>, o, st, steps);
 }
 
 }  // namespace

@@ -21,10 +21,7 @@ constexpr size_t kAlign = 256;
 constexpr int64_t kMaxDim = 1 << 22;       // 32-bit offsets of the operand loads: 256 rows of 2^22 fp16 words
 // Matrices step together (a cluster: every kernel of the iteration is one launch over it) up to this many elements; the
 // next cluster reuses the workspace.
-#ifndef CLU
-#define CLU 29
-#endif
-constexpr int64_t kClusterElements = (int64_t)1 << CLU;
+constexpr int64_t kClusterElements = (int64_t)1 << 29;
 // Elements behind one partial sum of squares, while those are fewer than kMuonParts.  With 16384 the odd matrix of six small
 // ones (201 x 327) took 24 us, the time of a thread's chain of single loads.
 constexpr int64_t kPartElements = 2048;
@@ -83,10 +80,7 @@ constexpr double kGrowth = 13.0, kLongGrowth = 160.0;
 bool long_first(Mode mode, int parts, bool step) { return parts == 1 && (mode == SMALL || step); }
 // In units of p^3 a step by itself costs 3 rho + 1 with rho = q / p, a segment of L steps 3 rho + 4 L - 3: the same for two
 // segments of 3 + 2 and five steps at rho = 1.  But a segment has more and smaller launches.
-#ifndef SEG_P
-#define SEG_P 512
-#endif
-constexpr int kSegmentRows = SEG_P;
+constexpr int kSegmentRows = 512;
 Mode mode_for(int p, int q) {
   if (p <= od::kNsSmall) return SMALL;
   return p >= kSegmentRows && 4 * (int64_t)q >= 5 * (int64_t)p ? SEGMENTS : STEP_BY_STEP;
@@ -95,8 +89,8 @@ Mode mode_for(int p, int q) {
 // Splits of the K range of a class's Gram matrices.  For the kernel that adds them up by itself (SMALL): its workgroup
 // reads 64 KB a split, about as long as two steps take, so the square root of the steps balances the two.  Otherwise
 // where the tiles leave most of the chip idle and the range is long: one round of workgroups, at least eight steps each.
-int splits_for(Mode mode, int p, int q, int nb, int parts) {
-  const int64_t steps = (int64_t)(up64(q) / od::kNsStep) * (parts == 2 ? 3 : 1);
+int splits_for(Mode mode, int p, int q, int nb) {
+  const int64_t steps = up64(q) / od::kNsStep;
   if (mode == SMALL) return (int)std::min<int64_t>(16, std::max<int64_t>(1, (int64_t)std::lround(std::sqrt(0.6 * (double)steps))));
   const int64_t n = (p + od::kNsSplitTile - 1) / od::kNsSplitTile, tiles = n * (n + 1) / 2 * nb;
   if (tiles >= 128 || steps < 16) return 0;
@@ -329,7 +323,7 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
     // 209 us a step, with launches of their own kernel in between 275.
     Mode mode = mode_for(c.p, c.q);
     if (mode == SMALL && !all_small) mode = STEP_BY_STEP;
-    const int splits = splits_for(mode, c.p, c.q, (int)c.members.size(), h->parts);
+    const int splits = splits_for(mode, c.p, c.q, (int)c.members.size());
     const Plan* const plan[2] = {&h->plans[0][splits > 0][mode], &h->plans[1][splits > 0][mode]};
     const int symmetric = std::max(plan[0]->symmetric, plan[1]->symmetric);
     const int64_t stride = h->parts * (2 * od::ns_y_plane(c.p, lq) + symmetric * od::ns_s_plane(c.p, lp)) + od::ns_partials(c.p, splits);
