@@ -627,12 +627,11 @@ __global__ __launch_bounds__(256) void k_ns_reduce(NsArgs args) {
 
 // All p x p work of a segment of steps for one matrix of p <= D, in one workgroup: S and P lie in LDS as two fp16 words a
 // value (22 bits, three products), T = P S and Z in the accumulators' registers, from where they change places with S.
-// A chain of products with a barrier after each, about 1.5 us at D = 128; as launches of their own the same products take
-// 8 us each.
+// A wave has one 32 x 32 block.  A chain of products with a barrier after each: bound by the latency of LDS and barriers.
 template <int D>
 struct NsSmallTile {
-  static constexpr int WI = 2, WJ = D / 32, NW = WI * WJ, THREADS = 64 * NW, FM = D / 64;      // wave tile D/2 x 32
-  static constexpr int ROWB = D * 2, PLANE = D * ROWB;
+  static constexpr int W = D / 32, THREADS = 64 * W * W;
+  static constexpr int PITCH = D * 2 + 16, PLANE = D * PITCH;      // an odd number of 16-byte slots: rows in different banks
   static constexpr int lds(int) { return 4 * PLANE; }
 };
 
@@ -645,123 +644,103 @@ __global__ __launch_bounds__(NsSmallTile<D>::THREADS, 1) void k_ns_small(NsJobs<
   uint16_t* slice = c.base + z * c.stride;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row0 = wave / TL::WJ * (D / 2), col0 = wave % TL::WJ * 32;
-  typedef f32x16 Acc[TL::FM];
+  // entry n of the accumulator: row `row`, column col0 + 8 (n / 4) + n % 4
+  const int row = wave / TL::W * 32 + (lane & 31), block = wave % TL::W * 32, col0 = block + 4 * (lane >> 5);
   char* const s_plane = lds;
   char* const p_plane = lds + 2 * TL::PLANE;
-  auto at = [](int row, int slot) { return row * TL::ROWB + ((slot ^ (D == 64 ? swz64(row) : row & 15)) << 4); };
-  // element e of entry v4 of accumulator i: row row0 + 32 i + lane % 32, column col0 + 8 v4 + 4 (lane / 32) + e
-  auto product = [&](const char* a, const char* b, Acc& out) {
+  auto product = [&](const char* a, const char* b) {
+    f32x16 hh, rest;
 #pragma unroll
-    for (int i = 0; i < TL::FM; ++i)
+    for (int n = 0; n < 16; ++n) hh[n] = rest[n] = 0.f;
+    const char* pa = a + row * TL::PITCH + (lane >> 5) * 16;
+    const char* pb = b + (block + (lane & 31)) * TL::PITCH + (lane >> 5) * 16;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) out[i][v] = 0.f;
-#pragma unroll 2
     for (int ks = 0; ks < D / 16; ++ks) {
-      const int kg = 2 * ks + (lane >> 5);
-      u32x4 bh = *reinterpret_cast<const u32x4*>(b + at(col0 + (lane & 31), kg));
-      u32x4 bl = *reinterpret_cast<const u32x4*>(b + TL::PLANE + at(col0 + (lane & 31), kg));
+      const u32x4 ah = *reinterpret_cast<const u32x4*>(pa + 32 * ks), al = *reinterpret_cast<const u32x4*>(pa + TL::PLANE + 32 * ks);
+      const u32x4 bh = *reinterpret_cast<const u32x4*>(pb + 32 * ks), bl = *reinterpret_cast<const u32x4*>(pb + TL::PLANE + 32 * ks);
+      hh = mfma_32x32x16<true>(bh, ah, hh);
+      rest = mfma_32x32x16<true>(bl, ah, rest);
+      rest = mfma_32x32x16<true>(bh, al, rest);
+    }
+    return hh + rest;
+  };
+  auto put = [&](char* plane, const f32x16& v, float scale) {
 #pragma unroll
-      for (int i = 0; i < TL::FM; ++i) {
-        const u32x4 ah = *reinterpret_cast<const u32x4*>(a + at(row0 + 32 * i + (lane & 31), kg));
-        const u32x4 al = *reinterpret_cast<const u32x4*>(a + TL::PLANE + at(row0 + 32 * i + (lane & 31), kg));
-        out[i] = mfma_32x32x16<true>(bl, ah, out[i]);
-        out[i] = mfma_32x32x16<true>(bh, al, out[i]);
-        out[i] = mfma_32x32x16<true>(bh, ah, out[i]);
-      }
+    for (int v4 = 0; v4 < 4; ++v4) {
+      uint32_t a[2], b[2];
+      split2<2>(scale * v[4 * v4], scale * v[4 * v4 + 1], a);
+      split2<2>(scale * v[4 * v4 + 2], scale * v[4 * v4 + 3], b);
+#pragma unroll
+      for (int part = 0; part < 2; ++part)
+        *reinterpret_cast<u32x2*>(plane + part * TL::PLANE + row * TL::PITCH + (col0 + 8 * v4) * 2) = u32x2{a[part], b[part]};
     }
   };
-  auto put = [&](char* plane, const Acc& v, float scale) {
-#pragma unroll
-    for (int i = 0; i < TL::FM; ++i)
-#pragma unroll
-      for (int v4 = 0; v4 < 4; ++v4) {
-        const int row = row0 + 32 * i + (lane & 31), col = col0 + 8 * v4 + 4 * (lane >> 5);
-        uint32_t a[2], b[2];
-        split2<2>(scale * v[i][4 * v4], scale * v[i][4 * v4 + 1], a);
-        split2<2>(scale * v[i][4 * v4 + 2], scale * v[i][4 * v4 + 3], b);
-#pragma unroll
-        for (int part = 0; part < 2; ++part)
-          *reinterpret_cast<u32x2*>(plane + part * TL::PLANE + at(row, col >> 3) + (col & 7) * 2) = u32x2{a[part], b[part]};
-      }
-  };
-  auto scaled = [](Acc& v, float f) {
-#pragma unroll
-    for (int i = 0; i < TL::FM; ++i)
-#pragma unroll
-      for (int n = 0; n < 16; ++n) v[i][n] *= f;
-  };
   // S, zero outside the matrix
-  Acc s, p, zz, t;
+  f32x16 s, p, zz, t;
   {
-    const float* in = reinterpret_cast<const float*>(slice + c.a);
+    const float* in = reinterpret_cast<const float*>(slice + c.a) + row * kNsSplitTile + col0;
 #pragma unroll
-    for (int i = 0; i < TL::FM; ++i)
-#pragma unroll
-      for (int n = 0; n < 16; ++n) s[i][n] = 0.f;
+    for (int n = 0; n < 16; ++n) s[n] = 0.f;
+#pragma unroll 4
     for (int split = 0; split < c.splits; ++split)
 #pragma unroll
-      for (int i = 0; i < TL::FM; ++i)
+      for (int v4 = 0; v4 < 4; ++v4) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(in + (int64_t)split * kNsSplitTile * kNsSplitTile + 8 * v4);
 #pragma unroll
-        for (int v4 = 0; v4 < 4; ++v4) {
-          const int row = row0 + 32 * i + (lane & 31), col = col0 + 8 * v4 + 4 * (lane >> 5);
-          const f32x4 x = *reinterpret_cast<const f32x4*>(in + (int64_t)split * kNsSplitTile * kNsSplitTile + row * kNsSplitTile + col);
+        for (int e = 0; e < 4; ++e) s[4 * v4 + e] += x[e];
+      }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[i][4 * v4 + e] += row < c.p && col + e < c.p ? x[e] : 0.f;
-        }
-    scaled(s, c.cc);
+    for (int n = 0; n < 16; ++n) s[n] = row < c.p && col0 + 8 * (n >> 2) + (n & 3) < c.p ? c.cc * s[n] : 0.f;
   }
   for (int l = 0; l < k.count; ++l) {
     if (l > 0) {
-      product(p_plane, s_plane, t);                       // T = P S
-      scaled(t, 1.f / (k.p[l - 1] * k.s[l - 1]));
+      t = product(p_plane, s_plane) * (1.f / (k.p[l - 1] * k.s[l - 1]));            // T = P S
       __syncthreads();
       if (l > 1) {
         put(s_plane, zz, k.z[l - 2]);
         __syncthreads();
-        product(p_plane, s_plane, zz);                    // Z = P Z
-        scaled(zz, 1.f / (k.p[l - 1] * k.z[l - 2]));
+        zz = product(p_plane, s_plane) * (1.f / (k.p[l - 1] * k.z[l - 2]));         // Z = P Z
         __syncthreads();
       } else {
-#pragma unroll
-        for (int i = 0; i < TL::FM; ++i) zz[i] = p[i];
+        zz = p;
       }
       put(s_plane, t, k.t[l - 1]);
       __syncthreads();
-      product(s_plane, p_plane, s);                       // S = T P
-      scaled(s, 1.f / (k.t[l - 1] * k.p[l - 1]));
+      s = product(s_plane, p_plane) * (1.f / (k.t[l - 1] * k.p[l - 1]));            // S = T P
       __syncthreads();
     }
     put(s_plane, s, k.s[l]);
     __syncthreads();
-    product(s_plane, s_plane, p);                         // P = a I + b S + c S S
-    const float ss = k.c[l] / (k.s[l] * k.s[l]);
+    p = product(s_plane, s_plane) * (k.c[l] / (k.s[l] * k.s[l]));                   // P = a I + b S + c S S
 #pragma unroll
-    for (int i = 0; i < TL::FM; ++i)
-#pragma unroll
-      for (int n = 0; n < 16; ++n) {
-        const int row = row0 + 32 * i + (lane & 31), col = col0 + 8 * (n >> 2) + 4 * (lane >> 5) + (n & 3);
-        p[i][n] = k.b[l] * s[i][n] + ss * p[i][n] + (row == col && row < c.p ? k.a[l] : 0.f);
-      }
+    for (int n = 0; n < 16; ++n) p[n] += k.b[l] * s[n] + (row == col0 + 8 * (n >> 2) + (n & 3) && row < c.p ? k.a[l] : 0.f);
     put(p_plane, p, k.p[l]);
     __syncthreads();
   }
   if (k.count > 1) {
     put(s_plane, zz, k.z[k.count - 2]);
     __syncthreads();
-    product(p_plane, s_plane, p);                         // Z = P Z
-    scaled(p, 1.f / (k.p[k.count - 1] * k.z[k.count - 2]));
+    p = product(p_plane, s_plane) * (1.f / (k.p[k.count - 1] * k.z[k.count - 2]));  // Z = P Z
   }
-  __syncthreads();
-  put(p_plane, p, k.z[k.count - 1]);
-  __syncthreads();
   // Z out, rows of pp columns
   const int64_t splane = (int64_t)c.p * c.lp;
-  for (int n = threadIdx.x; n < c.p * (pp / 8); n += TL::THREADS) {
-    const int row = n / (pp / 8), slot = n % (pp / 8);
 #pragma unroll
-    for (int part = 0; part < PARTS; ++part)
-      *reinterpret_cast<u32x4*>(slice + c.out + part * splane + (int64_t)row * c.lp + 8 * slot) = *reinterpret_cast<const u32x4*>(p_plane + part * TL::PLANE + at(row, slot));
+  for (int v4 = 0; v4 < 4; ++v4) {
+    const int col = col0 + 8 * v4;
+    uint32_t a[PARTS], b[PARTS];
+    const float f = k.z[k.count - 1];
+    split2<PARTS>(f * p[4 * v4], f * p[4 * v4 + 1], a);
+    split2<PARTS>(f * p[4 * v4 + 2], f * p[4 * v4 + 3], b);
+    if (row < c.p) {
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part) *reinterpret_cast<u32x2*>(slice + c.out + part * splane + (int64_t)row * c.lp + col) = u32x2{a[part], b[part]};
+    }
+  }
+  // columns D .. pp, which no block holds
+  for (int n = threadIdx.x; n < c.p * ((pp - D) / 8); n += TL::THREADS) {
+    const int r = n / ((pp - D) / 8), slot = n % ((pp - D) / 8);
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) *reinterpret_cast<u32x4*>(slice + c.out + part * splane + (int64_t)r * c.lp + D + 8 * slot) = u32x4{0u, 0u, 0u, 0u};
   }
 }
 
@@ -977,16 +956,23 @@ namespace {
 
 template <int D, int PARTS>
 hipError_t small_of(const NsArgs& a, const NsSteps& steps, hipStream_t st) {
-  const NsJobs<kNsClasses> o = laid_out<kNsClasses>(a, [](const NsJob& c) { return (c.p <= 64) == (D == 64); }, [](const NsJob&) { return 1; });
+  const NsJobs<kNsClasses> o = laid_out<kNsClasses>(a, [](const NsJob& c) { return (c.p + 31) / 32 * 32 == D; }, [](const NsJob&) { return 1; });
   return go<NsSmallTile<D>, PARTS>(k_ns_small<D, PARTS>, o, st, steps);
+}
+
+template <int PARTS>
+hipError_t small_sizes(const NsArgs& a, const NsSteps& steps, hipStream_t st) {
+  hipError_t rc = small_of<32, PARTS>(a, steps, st);
+  if (rc == hipSuccess) rc = small_of<64, PARTS>(a, steps, st);
+  if (rc == hipSuccess) rc = small_of<96, PARTS>(a, steps, st);
+  if (rc == hipSuccess) rc = small_of<128, PARTS>(a, steps, st);
+  return rc;
 }
 
 }  // namespace
 
 hipError_t launch_ns_small(const NsArgs& a, const NsSteps& steps, int parts, hipStream_t st) {
-  const hipError_t rc = parts == 2 ? small_of<64, 2>(a, steps, st) : small_of<64, 1>(a, steps, st);
-  if (rc != hipSuccess) return rc;
-  return parts == 2 ? small_of<128, 2>(a, steps, st) : small_of<128, 1>(a, steps, st);
+  return parts == 2 ? small_sizes<2>(a, steps, st) : small_sizes<1>(a, steps, st);
 }
 
 hipError_t launch_ns_final(const NsArgs& a, const MuonTables& t, int parts, bool update, float keep, float lr, bool x_bf16, hipStream_t st) {

@@ -86,6 +86,11 @@ Mode mode_for(int p, int q) {
   return p >= kSegmentRows && 4 * (int64_t)q >= 5 * (int64_t)p ? SEGMENTS : STEP_BY_STEP;
 }
 
+// In fast precision the orthogonalisation takes two words where that costs next to nothing, in sets so small that launches
+// take longer than their products (sum of p^2 q up to this): O then leaves with the error of its own rounding alone.  With one
+// word O of 400 x 600 is 1.95e-3 off before bf16's 1.7e-3.  The step, whose X takes lr O, keeps one.
+constexpr int64_t kTwoWordWork = (int64_t)1 << 29;
+
 // Splits of the K range of a class's Gram matrices.  For the kernel that adds them up by itself (SMALL): its workgroup
 // reads 64 KB a split, about as long as two steps take, so the square root of the steps balances the two.  Otherwise
 // where the tiles leave most of the chip idle and the range is long: one round of workgroups, at least eight steps each.
@@ -105,7 +110,7 @@ int exponent_for(double bound) { return 13 - (int)std::ceil(std::log2(bound)); }
 struct orthdion_muon_ctx {
   std::vector<orthdion_muon_matdesc> mats;
   orthdion_muon_config cfg;
-  int parts;
+  int parts[2];                            // words of a value: of the orthogonalisation, of the step
   Plan plans[2][2][kModes];                // [step][Gram matrices in partial sums][mode]
   int first_exp;                           // power of two of the scaled input
   std::vector<int> order;                  // table row -> matrix
@@ -296,11 +301,6 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
   h->first_exp = exponent_for(steps[0].top);
   const bool exact = cfg->precision == ORTHDION_PREC_EXACT ||
                      (cfg->precision == ORTHDION_PREC_AUTO && !(cfg->x_dtype == ORTHDION_BF16 && cfg->g_dtype == ORTHDION_BF16));
-  h->parts = exact ? 2 : 1;
-  for (int step = 0; step < 2; ++step)
-    for (int split = 0; split < 2; ++split)
-      for (int mode = 0; mode < kModes; ++mode) plan_jobs(steps, (Mode)mode, split != 0, h->parts, step != 0, &h->plans[step][split][mode]);
-
   // classes in order of first appearance
   struct Shape { int p, q, tall; std::vector<int> members; };
   std::vector<Shape> classes;
@@ -313,6 +313,13 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
   }
   bool all_small = true;
   for (const Shape& c : classes) all_small = all_small && mode_for(c.p, c.q) == SMALL;
+  double work = 0.0;
+  for (const Shape& c : classes) work += (double)c.p * c.p * c.q * (double)c.members.size();
+  h->parts[0] = exact || (!all_small && work <= (double)kTwoWordWork) ? 2 : 1;
+  h->parts[1] = exact ? 2 : 1;
+  for (int step = 0; step < 2; ++step)
+    for (int split = 0; split < 2; ++split)
+      for (int mode = 0; mode < kModes; ++mode) plan_jobs(steps, (Mode)mode, split != 0, h->parts[step], step != 0, &h->plans[step][split][mode]);
   // clusters
   int64_t held = 0;
   size_t slices = 0, most = 0;
@@ -326,7 +333,7 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
     const int splits = splits_for(mode, c.p, c.q, (int)c.members.size());
     const Plan* const plan[2] = {&h->plans[0][splits > 0][mode], &h->plans[1][splits > 0][mode]};
     const int symmetric = std::max(plan[0]->symmetric, plan[1]->symmetric);
-    const int64_t stride = h->parts * (2 * od::ns_y_plane(c.p, lq) + symmetric * od::ns_s_plane(c.p, lp)) + od::ns_partials(c.p, splits);
+    const int64_t stride = h->parts[0] * (2 * od::ns_y_plane(c.p, lq) + symmetric * od::ns_s_plane(c.p, lp)) + od::ns_partials(c.p, splits);
     for (size_t done = 0; done < c.members.size();) {
       if (h->clusters.empty() || held + elements > kClusterElements || (int)h->clusters.back().classes.size() == od::kNsClasses) {
         h->clusters.push_back(Cluster{});
@@ -400,7 +407,7 @@ static int muon_run(orthdion_muon_handle h, void* const* X, const void* const* G
                      reinterpret_cast<double*>(ws + h->off_partials), reinterpret_cast<int*>(ws + h->off_info)};
   const bool gbf = h->cfg.g_dtype == ORTHDION_BF16, xbf = h->cfg.x_dtype == ORTHDION_BF16, nesterov = h->cfg.nesterov != 0;
   const float keep = (float)(1.0 - (double)h->cfg.lr * (double)h->cfg.weight_decay);
-  const int parts = h->parts;
+  const int parts = h->parts[update];
   for (const Cluster& cl : h->clusters) {
     NsArgs args;
     auto add = [&](const Class& c, const PlannedJob& job) {
