@@ -372,7 +372,7 @@ int orthdion_muon_destroy(orthdion_muon_handle h);
 typedef struct orthdion_adamw_ctx* orthdion_adamw_handle;
 
 typedef struct {
-  int64_t length;         /* below 2^42 */
+  int64_t length;         /* below 2^35 */
   float lr_scale, weight_decay;
 } orthdion_adamw_desc;
 

@@ -562,6 +562,7 @@ class Muon:
             nesterov, coeffs, mu, lr, weight_decay, eps, _per_item("scale", scale, self.nmat), self.lds)
         self.workspace_bytes = orthdion_muon_workspace_bytes(self.handle)
         self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
+        self._home = torch.cuda.current_stream(self.workspace.device).cuda_stream if self.workspace.is_cuda else 0
 
     def _pointers(self, name: str, seq, dtype, which: int) -> List[int]:
         """Addresses of a list of tensors, after the checks that raw addresses cannot have: one wrong type, shape, stride or
@@ -586,7 +587,17 @@ class Muon:
         return [t.data_ptr() for t in seq]
 
     def _stream(self, stream) -> int:
-        return stream if stream is not None else self._torch.cuda.current_stream(self.workspace.device).cuda_stream
+        """The stream of a call.  The workspace belongs to the stream it was made on: another one is noted, so that its memory is
+        not given away while that stream still works on it."""
+        torch = self._torch
+        if stream is None:
+            used = torch.cuda.current_stream(self.workspace.device)
+            stream = used.cuda_stream
+        elif stream != self._home:
+            used = torch.cuda.ExternalStream(stream, device=self.workspace.device)
+        if stream != self._home and not torch.cuda.is_current_stream_capturing():
+            self.workspace.record_stream(used)
+        return stream
 
     def step(self, X, G, M, stream=None) -> None:
         """One optimizer step: X and M are updated in place."""

@@ -15,6 +15,10 @@
 #include "../../include/orthdion.h"
 #include "od_common.h"
 
+// A launch has fewer than 2^32 threads.
+constexpr int64_t kMostBlocks = (1 << 24) - 1;
+constexpr int64_t kMostLength = (int64_t)1 << 35;
+
 namespace od {
 
 constexpr int kAdamChunk = 56;             // tensors of a launch: their records fill the 4 KB of its arguments
@@ -148,7 +152,7 @@ static int adamw_create(orthdion_adamw_handle* out, const orthdion_adamw_desc* t
   if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0)) return ORTHDION_E_INVALID_ARG;
   if (!std::isfinite(cfg->lr) || !std::isfinite(cfg->eps) || cfg->eps < 0.f) return ORTHDION_E_INVALID_ARG;
   for (int i = 0; i < count; ++i) {
-    if (tensors[i].length < 0 || tensors[i].length >= ((int64_t)1 << 42)) return ORTHDION_E_BAD_SHAPE;
+    if (tensors[i].length < 0 || tensors[i].length >= kMostLength) return ORTHDION_E_BAD_SHAPE;
     if (!std::isfinite(tensors[i].weight_decay) || !std::isfinite(tensors[i].lr_scale)) return ORTHDION_E_INVALID_ARG;
   }
   orthdion_adamw_ctx* h = new (std::nothrow) orthdion_adamw_ctx();
@@ -216,11 +220,10 @@ extern "C" int orthdion_adamw_step(orthdion_adamw_handle h, void* const* X, cons
     a->blocks = 0;
     return hipGetLastError();
   };
-  constexpr int64_t kMostBlocks = 1 << 30;
   for (int i = 0; i < total; ++i) {
     const orthdion_adamw_desc& d = h->tensors[i];
     if (d.length == 0) continue;
-    // tensors beyond 2^42 are refused, so the workgroups of one always fit a launch
+    // the workgroups of one tensor always fit a launch
     const int64_t need = (d.length + kAdamSpan - 1) / kAdamSpan;
     if (a->count == kAdamChunk || a->blocks + need > kMostBlocks)
       if (flush(false) != hipSuccess) return ORTHDION_E_HIP;

@@ -31,7 +31,8 @@ struct MuonMat {                           // one matrix, as the elementwise ker
   int m, n;
   int64_t ldx, ldg, ldm;
   float scale;                             // of its update
-  int blocks;                              // partial sums
+  int blocks;                              // partial sums: row ranges times column ranges
+  int col_ranges;
 };
 
 // What a launch computes for one class: nb matrices of p x q (or q x p where tall).

@@ -57,7 +57,7 @@ OD_DEV double block_sum(double v, double* lds) {
   return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-// One workgroup: a range of rows of one matrix.  HBM bound: G read, M read and written.
+// One workgroup: a range of rows and columns of one matrix.  HBM bound: G read, M read and written.
 template <bool GBF>
 __global__ __launch_bounds__(256) void k_muon_begin(MuonChunk chunk, MuonTables t, int mat0, float mu, int nesterov) {
   __shared__ double lds[4];
@@ -69,22 +69,24 @@ __global__ __launch_bounds__(256) void k_muon_begin(MuonChunk chunk, MuonTables 
     t.entries[mat0 + z] = e;
     const_cast<MuonMat*>(t.mats)[mat0 + z] = a;
   }
-  const int64_t rows = ((int64_t)a.m + a.blocks - 1) / a.blocks;
-  const int64_t r0 = blockIdx.x * rows, r1 = min((int64_t)a.m, r0 + rows);
+  const int row_ranges = a.blocks / a.col_ranges, ri = blockIdx.x / a.col_ranges, ci = blockIdx.x % a.col_ranges;
+  const int64_t rows = ((int64_t)a.m + row_ranges - 1) / row_ranges;
+  const int64_t r0 = ri * rows, r1 = min((int64_t)a.m, r0 + rows);
+  const int cols = ((a.n + 7) / 8 + a.col_ranges - 1) / a.col_ranges * 8, n0 = min(a.n, ci * cols), n1 = min(a.n, n0 + cols);
   double sum = 0.0;
   const bool vec = rows_aligned(e.G, a.ldg) && (e.M == nullptr || rows_aligned(e.M, a.ldm));
   // threads side by side along a row: the power of two at or above its items, so that narrow rows share a wave
-  const int wide = vec ? a.n / 8 : 0;                       // whole groups of eight
+  const int wide = vec ? (n1 - n0) / 8 : 0;                 // whole groups of eight
   auto spread = [](int items) { int s = 1; while (s < 256 && s < items) s <<= 1; return s; };
   if (wide > 0) {
     const int tx = spread(wide), x = threadIdx.x & (tx - 1), y = threadIdx.x / tx, ty = 256 / tx;
     for (int64_t r = r0 + y; r < r1; r += ty)
       for (int c = x; c < wide; c += tx) {
         float g[8];
-        load8<GBF>(e.G, r * a.ldg + 8 * c, g);
+        load8<GBF>(e.G, r * a.ldg + n0 + 8 * c, g);
         if (e.M) {
           float m[8];
-          f32x4* mp = reinterpret_cast<f32x4*>(e.M + r * a.ldm + 8 * c);
+          f32x4* mp = reinterpret_cast<f32x4*>(e.M + r * a.ldm + n0 + 8 * c);
           SrcF32::unpack8(SrcF32::Raw8{mp[0], mp[1]}, m);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
@@ -100,11 +102,11 @@ __global__ __launch_bounds__(256) void k_muon_begin(MuonChunk chunk, MuonTables 
         }
       }
   }
-  const int c0 = 8 * wide, rest = a.n - c0;
+  const int c0 = n0 + 8 * wide, rest = n1 - c0;
   if (rest > 0) {
     const int tx = spread(rest), x = threadIdx.x & (tx - 1), y = threadIdx.x / tx, ty = 256 / tx;
     for (int64_t r = r0 + y; r < r1; r += ty)
-      for (int c = c0 + x; c < a.n; c += tx) {
+      for (int c = c0 + x; c < n1; c += tx) {
         const float g = load_elem<GBF>(e.G, r * a.ldg + c);
         float b = g;
         if (e.M) {

@@ -96,7 +96,7 @@ constexpr int64_t kTwoWordWork = (int64_t)1 << 29;
 // where the tiles leave most of the chip idle and the range is long: one round of workgroups, at least eight steps each.
 int splits_for(Mode mode, int p, int q, int nb) {
   const int64_t steps = up64(q) / od::kNsStep;
-  if (mode == SMALL) return (int)std::min<int64_t>(16, std::max<int64_t>(1, (int64_t)std::lround(std::sqrt(0.6 * (double)steps))));
+  if (mode == SMALL) return (int)std::min<int64_t>(64, std::max<int64_t>(1, (int64_t)std::lround(std::sqrt(0.6 * (double)steps))));
   const int64_t n = (p + od::kNsSplitTile - 1) / od::kNsSplitTile, tiles = n * (n + 1) / 2 * nb;
   if (tiles >= 128 || steps < 16) return 0;
   return (int)std::min<int64_t>((256 + tiles - 1) / tiles, steps / 8);
@@ -355,9 +355,11 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
       for (int k = 0; k < take; ++k) {
         const int i = c.members[done + k];
         const orthdion_muon_matdesc& d = mats[i];
-        const int64_t parts = std::min<int64_t>({(d.m * d.n + kPartElements - 1) / kPartElements, od::kMuonParts, d.m});
+        // rows are dealt out first; a matrix of few rows is cut across its columns too, in ranges of a multiple of 8
+        const int64_t want = std::min<int64_t>((d.m * d.n + kPartElements - 1) / kPartElements, od::kMuonParts);
+        const int64_t rows = std::min<int64_t>(want, d.m), cols = std::min<int64_t>(want / rows, (d.n + 7) / 8);
         h->order.push_back(i);
-        h->table.push_back(MuonMat{(int)d.m, (int)d.n, d.ldx, d.ldg, d.ldm, d.scale, (int)parts});
+        h->table.push_back(MuonMat{(int)d.m, (int)d.n, d.ldx, d.ldg, d.ldm, d.scale, (int)(rows * cols), (int)cols});
       }
       cl.count += take;
       held += take * elements;

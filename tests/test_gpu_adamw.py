@@ -202,3 +202,20 @@ def test_training_step_of_a_small_model_in_one_graph():
             assert np.allclose(host([params[2 + k]])[0], wx, rtol=32 * U, atol=32 * U * 0.1)
             assert np.allclose(host([second[k]])[0], wv, rtol=8 * U, atol=1e-44)
         assert counter.tolist() == [t, 0]
+
+
+def test_a_tensor_beyond_32_bit_offsets():
+    import torch
+    n = 2 ** 31 + 4099
+    gen = torch.Generator(device="cuda:0").manual_seed(0)
+    X, G = (torch.empty(n, device="cuda:0", dtype=torch.bfloat16).normal_(0, 0.1, generator=gen) for _ in range(2))
+    M, V = (torch.zeros(n, device="cuda:0") for _ in range(2))
+    spots = [slice(0, 64), slice(2 ** 30 - 32, 2 ** 30 + 32), slice(2 ** 31 - 32, 2 ** 31 + 32), slice(n - 64, n)]
+    before = [[host([t[s]])[0] for t in (X, M, V)] for s in spots]
+    grads = [host([G[s]])[0] for s in spots]
+    counter = torch.zeros(2, device="cuda:0", dtype=torch.int32)
+    binding.AdamW([n], x_dtype="bf16", lr=0.01).step([X], [G], [M], [V], counter)
+    f = lambda v: float(np.float32(v))
+    for s, b, g in zip(spots, before, grads):
+        check(([X[s]], [M[s]], [V[s]]), [[b[0]], [b[1]], [b[2]]], [g], 1, [f(0.01)], 0.9, 0.999, f(1e-8), [0.0], "bf16")
+    assert bool(((V > 0) == (G != 0)).all())          # no element was left out

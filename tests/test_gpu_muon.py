@@ -82,7 +82,7 @@ def check(got, want, tol):
 
 
 SHAPES = [(1, 1), (1, 7), (5, 1), (3, 3), (2, 300), (300, 2), (8, 64), (64, 64), (65, 63), (127, 129), (129, 127), (128, 256),
-          (200, 328), (130, 1000), (1000, 130), (257, 513), (640, 384), (31, 2500), (512, 4104)]
+          (200, 328), (130, 1000), (1000, 130), (257, 513), (640, 384), (31, 2500), (512, 4104), (1, 100003), (50001, 3)]
 
 
 @pytest.mark.parametrize("shape", SHAPES)
@@ -185,7 +185,7 @@ def test_zero_tiny_huge_and_non_finite_matrices_leave_the_others_alone():
     assert torch.equal(O[0], O[7])
     alone = binding.Muon([shape], x_dtype="f32", eps=0.0)
     alone.orthogonalise([A[0]], [O[1]])
-    assert torch.equal(O[0], O[1])               # a matrix's bits do not depend on what is beside it
+    assert torch.equal(O[0], O[1])               # nothing of the matrices beside it
 
 
 def test_eps_damps_small_matrices():
@@ -290,3 +290,51 @@ def test_parts_of_a_fused_projection():
         check(o, newton_schulz(host, QUINTIC), tolerance(host, QUINTIC, False, "bf16"))
     with pytest.raises(ValueError):
         opt.orthogonalise([t.contiguous() for t in cut(G)], cut(X))
+
+
+@pytest.mark.parametrize("shape,count", [((768, 768), 16), ((2000, 700), 3), ((520, 1300), 6), ((1100, 1100), 1), ((150, 9000), 2), ((90, 6000), 3),
+                                         ((600, 150), 40)])
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+def test_every_tile_and_plan(shape, count, x):
+    """Sizes at which 64, 128 and 256 wide tiles, partial sums, shared Gram matrices and the small-matrix kernel are chosen;
+    three matrices of each set, all of them different."""
+    import torch
+    gen = torch.Generator().manual_seed(shape[0] + count)
+    dt = types(torch, x)
+    A = [torch.randn(*shape, generator=gen).to("cuda:0", dt) for _ in range(count)]
+    O = [torch.empty_like(a) for a in A]
+    M = [torch.zeros(*shape, device="cuda:0") for _ in range(count)]
+    X = [torch.zeros(*shape, device="cuda:0") for _ in range(count)]
+    opt = binding.Muon([shape] * count, x_dtype=x)
+    opt.orthogonalise(A, O)
+    step = binding.Muon([shape] * count, x_dtype="f32", g_dtype=x, precision="fast" if x == "bf16" else "exact", mu=0.0, lr=-1.0, scale="none")
+    step.step(X, A, M)                      # X = O of the step's own plan
+    assert opt.info() == [0] * count and step.info() == [0] * count
+    for k in sorted({0, count // 2, count - 1}):
+        host = A[k].double().cpu().numpy()
+        want = newton_schulz(host, QUINTIC)
+        check(O[k], want, tolerance(host, QUINTIC, x == "f32", x))
+        # the step's first three steps may share a Gram matrix, whose rounding counts twelve times as much in the third
+        # (the published coefficients' max |P|^2): twice the sum over all steps
+        check(X[k], want, 2 * tolerance(host, QUINTIC, x == "f32", "f32"))
+
+
+def test_rows_beyond_32_bit_offsets():
+    """A narrow matrix whose rows lie so far apart that its last ones start beyond 2^32 bytes and 2^31 elements."""
+    import torch
+    m, n, ld = 66000, 24, 33000
+    assert (m - 1) * ld > 2 ** 31
+    gen = torch.Generator(device="cuda:0").manual_seed(5)
+    G, X, M = (torch.zeros((m - 1) * ld + n, device="cuda:0", dtype=dt).as_strided((m, n), (ld, 1)) for dt in
+               (torch.bfloat16, torch.bfloat16, torch.float32))
+    dense = [torch.randn(m, n, device="cuda:0", generator=gen).to(t.dtype) for t in (G, X, M)]
+    for far, near in zip((G, X, M), dense):
+        far.copy_(near)
+    binding.Muon([(m, n)], x_dtype="bf16", lds=[(ld,) * 3]).step([X], [G], [M])
+    g, x, mom = dense
+    binding.Muon([(m, n)], x_dtype="bf16").step([x], [g], [mom])
+    assert torch.equal(X, x) and torch.equal(M, mom)
+    o = torch.zeros(m, n, device="cuda:0")
+    binding.Muon([(m, n)], x_dtype="f32").orthogonalise([g.float()], [o])
+    host = g.double().cpu().numpy()
+    check(o, newton_schulz(host, QUINTIC), tolerance(host, QUINTIC, True, "f32"))
