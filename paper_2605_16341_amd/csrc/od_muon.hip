@@ -746,18 +746,14 @@ __global__ __launch_bounds__(NsSmallTile<D>::THREADS, 1) void k_ns_small(NsJobs<
   }
 }
 
-// O = P Y into the caller's matrix, or its update
+// O = P Y into the caller's matrix, or its update.  TALL: the accumulators lie the other way round, so that either way a lane
+// has four consecutive columns of a row of the caller's matrix.
 template <class TL, int PARTS, bool XBF, bool TALL>
-__global__ __launch_bounds__(TL::THREADS, TL::blocks(PARTS)) void k_ns_final(NsArgs args, MuonTables t, int update, float keep, float lr) {
-  extern __shared__ __align__(16) char lds[];
+OD_DEV void ns_final_tile(const NsJob& c, int z, int ti, int tj, const MuonTables& t, int update, float keep, float lr, char* lds) {
   constexpr int T = TL::T;
-  const int bid = xcd_contiguous(blockIdx.x, args.total);
-  const NsJob c = args.j[ns_job(args, bid)];
   const float scale = c.cc;
-  const int pp = up64(c.p), qq = up64(c.q), ni = (c.p + T - 1) / T, nj = (c.q + T - 1) / T, local = bid - c.first;
+  const int pp = up64(c.p), qq = up64(c.q);
   const int64_t yplane = (int64_t)pp * c.lq, splane = (int64_t)c.p * c.lp;
-  const int z = quotient(local, ni * nj), tl = local - z * (ni * nj);
-  const int tj = quotient(tl, ni), ti = tl - tj * ni;
   uint16_t* slice = c.base + z * c.stride;
   const NsOperand A{slice + c.a + (int64_t)ti * T * c.lp, splane, c.lp, c.p - ti * T}, B{slice + c.b + tj * T, yplane, c.lq, qq - tj * T};
   f32x16 acc[TL::FM][TL::FN];
@@ -822,6 +818,18 @@ __global__ __launch_bounds__(TL::THREADS, TL::blocks(PARTS)) void k_ns_final(NsA
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   });
+}
+
+template <class TL, int PARTS, bool XBF>
+__global__ __launch_bounds__(TL::THREADS, TL::blocks(PARTS)) void k_ns_final(NsArgs args, MuonTables t, int update, float keep, float lr) {
+  extern __shared__ __align__(16) char lds[];
+  const int bid = xcd_contiguous(blockIdx.x, args.total);
+  const NsJob c = args.j[ns_job(args, bid)];
+  const int ni = (c.p + TL::T - 1) / TL::T, nj = (c.q + TL::T - 1) / TL::T, local = bid - c.first;
+  const int z = quotient(local, ni * nj), tl = local - z * (ni * nj);
+  const int tj = quotient(tl, ni), ti = tl - tj * ni;
+  if (c.tall) ns_final_tile<TL, PARTS, XBF, true>(c, z, ti, tj, t, update, keep, lr, lds);
+  else ns_final_tile<TL, PARTS, XBF, false>(c, z, ti, tj, t, update, keep, lr, lds);
 }
 
 // ------------------------------------------------------------------------------------
@@ -892,12 +900,13 @@ int tiles_of(const NsJob& c) {
   return c.kind == NS_APPLY ? n * ceil_div(c.q, T) : c.kind == NS_FULL ? n * n : n * (n + 1) / 2 * (c.splits > 0 ? c.splits : 1);
 }
 
-// f with the tile for these jobs: the one with the least time by what a step of 64 k takes, in us.  64 x 64: 0.43 while every
-// workgroup has a CU, 0.36 for each on a CU beyond that (two at a time); 128 x 128: 0.7 alone on a CU, 1.1 for two side by
-// side, 1.4 where that happens everywhere and the clock gives way; 256 x 256: 1.65, 2.0 with most CUs at work.  Measured on
-// products of 264 x 264 to 3000 x 3000, 1 to 16 matrices: the rule takes the fastest of the three or one within 10 %.
+// f with the tile for these jobs: the one with the least time by what a step of 64 k takes, in us.
+// One word: 64 x 64 0.43 while every workgroup has a CU, 0.36 for each on a CU beyond that; 128 x 128 0.7 alone on a CU, 1.1 for two
+// side by side, 1.4 where that happens everywhere and the clock gives way; 256 x 256 1.65, 2.0 with most CUs at work.
+// Two words: 0.8 and 0.65; 1.7 a round (one workgroup fits a CU); 5.2 and 6.3.
+// Measured on products of 264 x 264 to 3000 x 3000, 1 to 16 matrices: the rule takes the fastest of the three or one within 10 %.
 template <class F>
-hipError_t with_tile(const NsArgs& a, F&& f) {
+hipError_t with_tile(const NsArgs& a, int parts, F&& f) {
   double n64 = 0.0, n128 = 0.0, n256 = 0.0;
   for (int k = 0; k < a.count; ++k) {
     if (a.j[k].splits > 0) return f(Small{});          // partial sums
@@ -906,18 +915,23 @@ hipError_t with_tile(const NsArgs& a, F&& f) {
     n256 += (double)a.j[k].nb * tiles_of<256>(a.j[k]);
   }
   const double rest = n128 - 512.0 * std::floor(n128 / 512.0);
-  const double t64 = std::max(0.43, 0.36 / 256.0 * n64);
-  const double t128 = 1.4 * std::floor(n128 / 512.0) + (rest == 0.0 ? 0.0 : rest <= 256.0 ? 0.7 : 1.1);
-  const double t256 = std::ceil(n256 / 256.0) * (n256 >= 200.0 ? 2.0 : 1.65);
+  double t64, t128, t256;
+  if (parts == 1) {
+    t64 = std::max(0.43, 0.36 / 256.0 * n64);
+    t128 = 1.4 * std::floor(n128 / 512.0) + (rest == 0.0 ? 0.0 : rest <= 256.0 ? 0.7 : 1.1);
+    t256 = std::ceil(n256 / 256.0) * (n256 >= 200.0 ? 2.0 : 1.65);
+  } else {
+    t64 = std::max(0.8, 0.65 / 256.0 * n64);
+    t128 = 1.7 * std::ceil(n128 / 256.0);
+    t256 = std::ceil(n256 / 256.0) * (n256 >= 200.0 ? 6.3 : 5.2);
+  }
   if (t64 <= t128 && t64 <= t256) return f(Tiny{});
   return t128 <= t256 ? f(Small{}) : f(Large{});
 }
 
 template <class TL, int PARTS, bool XBF>
 hipError_t final_of(const NsArgs& a, const MuonTables& t, bool update, float keep, float lr, hipStream_t st) {
-  const hipError_t rc = go<TL, PARTS>(k_ns_final<TL, PARTS, XBF, false>, laid_out(a, [](const NsJob& c) { return !c.tall; }, tiles_of<TL::T>), st, t, (int)update, keep, lr);
-  if (rc != hipSuccess) return rc;
-  return go<TL, PARTS>(k_ns_final<TL, PARTS, XBF, true>, laid_out(a, [](const NsJob& c) { return c.tall != 0; }, tiles_of<TL::T>), st, t, (int)update, keep, lr);
+  return go<TL, PARTS>(k_ns_final<TL, PARTS, XBF>, laid_out(a, any, tiles_of<TL::T>), st, t, (int)update, keep, lr);
 }
 
 template <class TL>
@@ -944,7 +958,7 @@ hipError_t launch_muon_scale(const NsArgs& a, const MuonTables& t, float mu, boo
 }
 
 hipError_t launch_ns_products(const NsArgs& a, int parts, hipStream_t st) {
-  return with_tile(a, [&](auto tile) { return products_of<decltype(tile)>(a, parts, st); });
+  return with_tile(a, parts, [&](auto tile) { return products_of<decltype(tile)>(a, parts, st); });
 }
 
 hipError_t launch_ns_reduce(const NsArgs& a, int parts, hipStream_t st) {
@@ -978,7 +992,7 @@ hipError_t launch_ns_small(const NsArgs& a, const NsSteps& steps, int parts, hip
 }
 
 hipError_t launch_ns_final(const NsArgs& a, const MuonTables& t, int parts, bool update, float keep, float lr, bool x_bf16, hipStream_t st) {
-  return with_tile(a, [&](auto tile) { return final_tiles<decltype(tile)>(a, t, parts, update, keep, lr, x_bf16, st); });
+  return with_tile(a, parts, [&](auto tile) { return final_tiles<decltype(tile)>(a, t, parts, update, keep, lr, x_bf16, st); });
 }
 
 }  // namespace od
