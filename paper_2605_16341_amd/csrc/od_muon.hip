@@ -432,9 +432,9 @@ OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const 
 
 // Writes a wave's tile of fp16 words 16 bytes a lane, with `mirror` the transpose too: 32 rows at a time through the
 // wave's own part of LDS.  `value(i, j, v4, row, col, x)`: the four values of accumulator (i, j) from entry 4 v4 on, the
-// first of them at row, col of the wave's tile.  Rows below `rows` and columns below `cols` are written, from `valid` on as zero.
-template <class TL, int PARTS, class V>
-OD_DEV void ns_store(char* lds, V&& value, uint16_t* out, int64_t plane, int ld, int row0, int col0, int rows, int cols,
+// first of them at row, col of the wave's tile; `ahead(i)` loads what they need for the accumulators i, 32 rows ahead.  Rows below `rows` and columns below `cols` are written, from `valid` on as zero.
+template <class TL, int PARTS, class L, class V>
+OD_DEV void ns_store(char* lds, L&& ahead, V&& value, uint16_t* out, int64_t plane, int ld, int row0, int col0, int rows, int cols,
                      int valid, bool mirror) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -449,8 +449,10 @@ OD_DEV void ns_store(char* lds, V&& value, uint16_t* out, int64_t plane, int ld,
     return w;
   };
   char* mine = lds + wave * (PARTS * PIECE);
+  ahead(std::integral_constant<int, 0>{});
   static_for<TL::FM>([&](auto ii) {
     constexpr int i = decltype(ii)::value;
+    if constexpr (i + 1 < TL::FM) ahead(std::integral_constant<int, i + 1>{});
     static_for<TL::FN * 4>([&](auto jj) {
       constexpr int j = decltype(jj)::value / 4, v4 = decltype(jj)::value % 4;
       const int r = lane & 31, c = 32 * j + 8 * v4 + 4 * (lane >> 5);
@@ -526,7 +528,7 @@ __global__ __launch_bounds__(TL::THREADS, TL::blocks(PARTS)) void k_ns_products(
     ns_product<TL, PARTS, true, true>(acc, A, B, pp, lds);
     __syncthreads();
     const int row0 = ti * T + wave / TL::WJ * TL::WTM, col0 = tj * T + wave % TL::WJ * TL::WTN;
-    ns_store<TL, PARTS>(lds, [&](auto i, auto j, auto v4, int, int, float* x) {
+    ns_store<TL, PARTS>(lds, [](auto) {}, [&](auto i, auto j, auto v4, int, int, float* x) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] = c.cc * acc[i][j][4 * v4 + e];
     }, slice + c.out, yplane, c.lq, row0, col0, c.p, qq, c.q, false);
@@ -560,24 +562,34 @@ __global__ __launch_bounds__(TL::THREADS, TL::blocks(PARTS)) void k_ns_products(
     __syncthreads();
     const int row0 = ti * T + wave / TL::WJ * TL::WTM, col0 = tj * T + wave % TL::WJ * TL::WTN;
     const uint16_t* E = slice + c.e;
-    ns_store<TL, PARTS>(lds, [&](auto i, auto j, auto v4, int r, int cl, float* x) {
-      float s[4] = {0.f, 0.f, 0.f, 0.f};
-      const int row = row0 + r, col = col0 + cl;
-      if (c.cb != 0.f && row < c.p && col < pp) {
+    const int lane = threadIdx.x & 63;
+    u32x2 word[2][PARTS][TL::FN][4];             // of e, for two blocks of 32 rows
+    ns_store<TL, PARTS>(lds, [&](auto i) {
+      constexpr int set = decltype(i)::value & 1;
+      const int row = min(row0 + 32 * i + (lane & 31), c.p - 1);
+      if (c.cb == 0.f) return;
 #pragma unroll
-        for (int part = 0; part < PARTS; ++part) {
-          const u32x2 w = *reinterpret_cast<const u32x2*>(E + part * splane + (int64_t)row * c.lp + col);
+      for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+        for (int j = 0; j < TL::FN; ++j)
+#pragma unroll
+          for (int v4 = 0; v4 < 4; ++v4)
+            word[set][part][j][v4] = *reinterpret_cast<const u32x2*>(E + part * splane + (int64_t)row * c.lp + min(col0 + 32 * j + 8 * v4 + 4 * (lane >> 5), pp - 4));
+    }, [&](auto i, auto j, auto v4, int r, int cl, float* x) {
+      const int row = row0 + r, col = col0 + cl;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = c.cc * acc[i][j][4 * v4 + e] + (row == col + e ? c.ca : 0.f);
+      if (c.cb != 0.f) {
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const uint32_t pair = w[e];          // a bit cast of a vector's element itself would take its first one
+            const uint32_t pair = word[i & 1][part][j][v4][e];      // a bit cast of a vector's element itself would take its first one
             const f16x2 h = __builtin_bit_cast(f16x2, pair);
-            s[2 * e] += (float)h[0];
-            s[2 * e + 1] += (float)h[1];
+            x[2 * e] += c.cb * (float)h[0];
+            x[2 * e + 1] += c.cb * (float)h[1];
           }
-        }
       }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = c.cc * acc[i][j][4 * v4 + e] + c.cb * s[e] + (row == col + e ? c.ca : 0.f);
     }, slice + c.out, splane, c.lp, row0, col0, c.p, pp, c.p, !full && ti != tj);
   }
 }
