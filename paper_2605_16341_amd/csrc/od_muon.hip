@@ -259,10 +259,10 @@ OD_DEV void static_for(F&& f) {
 }
 
 OD_DEV int swz64(int row) { return (row >> 1) & 7; }
-// the 16-byte slots by which row k of a tile with k down its columns is rotated: rows of 128 bytes lie in alternate halves
-// of the 256 bytes of all banks already
+// what the 16-byte slots of row k of a tile with k down its columns are XORed with: rows of 128 or 384 bytes lie in alternate
+// halves of the 256 bytes of all banks already
 template <int T>
-OD_DEV int swz_down(int k) { return T == 64 ? (k & 2) << 1 : (k & 3) << 2; }
+OD_DEV int swz_down(int k) { return T % 128 ? (k & 2) << 1 : (k & 3) << 2; }
 
 struct NsOperand {
   const uint16_t* p;      // tile's first row (TRB: the tile's first column is in `edge`)
@@ -303,7 +303,7 @@ OD_DEV void ns_product(f32x16 (&acc)[TL::FM][TL::FN], const NsOperand& A, const 
     va[j] = (uint32_t)min(row, A.rows - 1) * (uint32_t)(A.ld * 2) + kg * 16;
     if constexpr (TRB) {
       constexpr int SLOTS = T / 8;                       // 16-byte groups of a row
-      const int k = chunk * (64 / SLOTS) + lane / SLOTS, cg = (lane % SLOTS) ^ swz_down<T>(k);
+      const int k = (chunk * 64 + lane) / SLOTS, cg = ((chunk * 64 + lane) % SLOTS) ^ swz_down<T>(k);
       vb[j] = (uint32_t)k * (uint32_t)(B.ld * 2) + min(cg * 8, B.rows - 8) * 2;
     } else {
       vb[j] = (uint32_t)min(row, B.rows - 1) * (uint32_t)(B.ld * 2) + kg * 16;
@@ -438,9 +438,10 @@ OD_DEV void ns_store(char* lds, L&& ahead, V&& value, uint16_t* out, int64_t pla
                      int valid, bool mirror) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  constexpr int ROWB = TL::WTN * 2, SL = ROWB / 16, PIECE = 32 * ROWB;       // bytes and 16-byte slots of a staged row
+  // 16-byte slots and bytes of a staged row, whose slots are rotated where they are a power of two, otherwise padded
+  constexpr int SL = TL::WTN / 8, ROWB = SL * 16 + (SL & (SL - 1) ? 16 : 0), PIECE = 32 * ROWB;
+  auto at = [](int r, int slot) { return r * ROWB + ((SL & (SL - 1) ? slot : slot ^ (SL == 8 ? swz64(r) : r & (SL - 1))) << 4); };
   static_assert(TL::NW * PARTS * PIECE <= TL::lds(PARTS), "staging");
-  auto swz = [](int r) { return SL == 8 ? swz64(r) : r & (SL - 1); };
   auto masked = [&](u32x4 w, int col) {
     if (col + 8 > valid) {
 #pragma unroll
@@ -465,7 +466,7 @@ OD_DEV void ns_store(char* lds, L&& ahead, V&& value, uint16_t* out, int64_t pla
       split2<PARTS>(x[2], x[3], b);
 #pragma unroll
       for (int part = 0; part < PARTS; ++part)
-        *reinterpret_cast<u32x2*>(mine + part * PIECE + r * ROWB + (((c >> 3) ^ swz(r)) << 4) + (c & 7) * 2) = u32x2{a[part], b[part]};
+        *reinterpret_cast<u32x2*>(mine + part * PIECE + at(r, c >> 3) + (c & 7) * 2) = u32x2{a[part], b[part]};
     });
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
@@ -474,8 +475,8 @@ OD_DEV void ns_store(char* lds, L&& ahead, V&& value, uint16_t* out, int64_t pla
       const char* piece = mine + part * PIECE;
 #pragma unroll
       for (int it = 0; it < SL / 2; ++it) {
-        const int r = it * (64 / SL) + lane / SL, slot = lane % SL;
-        const u32x4 w = *reinterpret_cast<const u32x4*>(piece + r * ROWB + ((slot ^ swz(r)) << 4));
+        const int r = (it * 64 + lane) / SL, slot = (it * 64 + lane) % SL;
+        const u32x4 w = *reinterpret_cast<const u32x4*>(piece + at(r, slot));
         const int row = row0 + 32 * i + r, col = col0 + 8 * slot;
         if (row < rows && col < cols) *reinterpret_cast<u32x4*>(o + (int64_t)row * ld + col) = masked(w, col);
       }
@@ -485,8 +486,8 @@ OD_DEV void ns_store(char* lds, L&& ahead, V&& value, uint16_t* out, int64_t pla
 #pragma unroll
         for (int cb = 0; cb < TL::WTN / 16; ++cb) {
           const int c = cb * 16 + 4 * (lane & 3), r = (lane >> 4) * 8 + ((lane & 15) >> 2);
-          const s16x4 h0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(piece + r * ROWB + (((c >> 3) ^ swz(r)) << 4) + (c & 7) * 2));
-          const s16x4 h1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(piece + (r + 4) * ROWB + (((c >> 3) ^ swz(r + 4)) << 4) + (c & 7) * 2));
+          const s16x4 h0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(piece + at(r, c >> 3) + (c & 7) * 2));
+          const s16x4 h1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(piece + at(r + 4, c >> 3) + (c & 7) * 2));
           const u32x2 l2 = __builtin_bit_cast(u32x2, h0), h2 = __builtin_bit_cast(u32x2, h1);
           const int row = col0 + cb * 16 + (lane & 15), col = row0 + 32 * i + (lane >> 4) * 8;
           if (row < rows && col < cols) *reinterpret_cast<u32x4*>(o + (int64_t)row * ld + col) = masked(u32x4{l2[0], l2[1], h2[0], h2[1]}, col);
@@ -903,6 +904,7 @@ hipError_t go(K* kernel, const NsJobs<N>& a, hipStream_t st, A... rest) {
 
 typedef NsTile<64, 2, 2> Tiny;
 typedef NsTile<128, 2, 2> Small;
+typedef NsTile<192, 2, 2> Mid;
 typedef NsTile<256, 2, 4> Large;
 static_assert(Small::T == kNsSplitTile, "partial sums are those of its tiles");
 
@@ -912,33 +914,43 @@ int tiles_of(const NsJob& c) {
   return c.kind == NS_APPLY ? n * ceil_div(c.q, T) : c.kind == NS_FULL ? n * n : n * (n + 1) / 2 * (c.splits > 0 ? c.splits : 1);
 }
 
-// f with the tile for these jobs: the one with the least time by what a step of 64 k takes, in us.
-// One word: 64 x 64 0.43 while every workgroup has a CU, 0.36 for each on a CU beyond that; 128 x 128 0.7 alone on a CU, 1.1 for two
-// side by side, 1.4 where that happens everywhere and the clock gives way; 256 x 256 1.65, 2.0 with most CUs at work.
-// Two words: 0.8 and 0.65; 1.7 a round (one workgroup fits a CU); 5.2 and 6.3.
-// Measured on products of 264 x 264 to 3000 x 3000, 1 to 16 matrices: the rule takes the fastest of the three or one within 10 %.
+// f with the tile for these jobs: the one with the least time in us by what a step of 64 k and a workgroup's beginning and
+// end take.  256 CUs; beyond one round of workgroups the last one counts half by what is in it, half as a whole one.
+// One word: 64 x 64 0.43 a step, 0.30 for each workgroup of a CU where there are more, and 4; 128 x 128 0.7 and 4 alone on a CU, 1.0
+// and 5 for two side by side, 1.2 where that happens everywhere and the clock gives way; 192 x 192 1.15 and 6, 1.43 in several
+// rounds; 256 x 256 1.7 and 8, 1.85 with most CUs at work.
+// Two words: 64 x 64 0.8 and 0.65, 128 x 128 1.7 a round (one workgroup fits a CU), 256 x 256 5.2 and 6.3 (three passes).
+// Measured on products of 264 x 264 to 4096 x 4096, 1 to 72 matrices: the rule takes the fastest or one within 10 %.
 template <class F>
 hipError_t with_tile(const NsArgs& a, int parts, F&& f) {
-  double n64 = 0.0, n128 = 0.0, n256 = 0.0;
+  double n64 = 0.0, n128 = 0.0, n192 = 0.0, n256 = 0.0, steps = 0.0;
   for (int k = 0; k < a.count; ++k) {
-    if (a.j[k].splits > 0) return f(Small{});          // partial sums
-    n64 += (double)a.j[k].nb * tiles_of<64>(a.j[k]);
-    n128 += (double)a.j[k].nb * tiles_of<128>(a.j[k]);
-    n256 += (double)a.j[k].nb * tiles_of<256>(a.j[k]);
+    const NsJob& j = a.j[k];
+    if (j.splits > 0) return f(Small{});               // partial sums
+    const double nb = j.nb, n = nb * tiles_of<256>(j);
+    n64 += nb * tiles_of<64>(j);
+    n128 += nb * tiles_of<128>(j);
+    n192 += nb * tiles_of<192>(j);
+    n256 += n;
+    steps += n * ceil_div(j.kind == NS_GRAM ? j.q : j.p, kNsStep);
   }
-  const double rest = n128 - 512.0 * std::floor(n128 / 512.0);
-  double t64, t128, t256;
+  const double s = steps / n256, pairs = std::floor(n128 / 512.0), rest = n128 - 512.0 * pairs;
+  auto rounds = [](double n) { return n <= 256.0 ? 1.0 : 0.5 * n / 256.0 + 0.5 * std::ceil(n / 256.0) + 0.15; };
+  double t64, t128, t192, t256;
   if (parts == 1) {
-    t64 = std::max(0.43, 0.36 / 256.0 * n64);
-    t128 = 1.4 * std::floor(n128 / 512.0) + (rest == 0.0 ? 0.0 : rest <= 256.0 ? 0.7 : 1.1);
-    t256 = std::ceil(n256 / 256.0) * (n256 >= 200.0 ? 2.0 : 1.65);
+    t64 = std::max(0.43, 0.30 / 256.0 * n64) * s + 4.0;
+    t128 = pairs * (1.2 * s + 5.0) + (rest == 0.0 ? 0.0 : rest <= 256.0 ? 0.7 * s + 4.0 : 1.0 * s + 5.0);
+    t192 = rounds(n192) * ((n192 <= 256.0 ? 1.15 : 1.43) * s + 6.0);
+    t256 = rounds(n256) * ((n256 < 200.0 ? 1.7 : 1.85) * s + 8.0);
   } else {
-    t64 = std::max(0.8, 0.65 / 256.0 * n64);
-    t128 = 1.7 * std::ceil(n128 / 256.0);
-    t256 = std::ceil(n256 / 256.0) * (n256 >= 200.0 ? 6.3 : 5.2);
+    t64 = std::max(0.8, 0.65 / 256.0 * n64) * s + 4.0;
+    t128 = std::ceil(n128 / 256.0) * (1.7 * s + 5.0);
+    t192 = INFINITY;
+    t256 = std::ceil(n256 / 256.0) * ((n256 < 200.0 ? 5.2 : 6.3) * s + 8.0);
   }
-  if (t64 <= t128 && t64 <= t256) return f(Tiny{});
-  return t128 <= t256 ? f(Small{}) : f(Large{});
+  t192 *= 1.07;                                        // the least even of the four: taken where it is clearly ahead
+  const double least = std::min(std::min(t64, t128), std::min(t192, t256));
+  return least == t64 ? f(Tiny{}) : least == t128 ? f(Small{}) : least == t192 ? f(Mid{}) : f(Large{});
 }
 
 template <class TL, int PARTS, bool XBF>
@@ -949,12 +961,17 @@ hipError_t final_of(const NsArgs& a, const MuonTables& t, bool update, float kee
 template <class TL>
 hipError_t products_of(const NsArgs& a, int parts, hipStream_t st) {
   const NsArgs o = laid_out(a, any, tiles_of<TL::T>);
-  return parts == 2 ? go<TL, 2>(k_ns_products<TL, 2>, o, st) : go<TL, 1>(k_ns_products<TL, 1>, o, st);
+  if constexpr (TL::T != 192) {
+    if (parts == 2) return go<TL, 2>(k_ns_products<TL, 2>, o, st);
+  }
+  return go<TL, 1>(k_ns_products<TL, 1>, o, st);
 }
 
 template <class TL>
 hipError_t final_tiles(const NsArgs& a, const MuonTables& t, int parts, bool update, float keep, float lr, bool x_bf16, hipStream_t st) {
-  if (parts == 2) return x_bf16 ? final_of<TL, 2, true>(a, t, update, keep, lr, st) : final_of<TL, 2, false>(a, t, update, keep, lr, st);
+  if constexpr (TL::T != 192) {
+    if (parts == 2) return x_bf16 ? final_of<TL, 2, true>(a, t, update, keep, lr, st) : final_of<TL, 2, false>(a, t, update, keep, lr, st);
+  }
   return x_bf16 ? final_of<TL, 1, true>(a, t, update, keep, lr, st) : final_of<TL, 1, false>(a, t, update, keep, lr, st);
 }
 
