@@ -164,7 +164,8 @@ __global__ __launch_bounds__(256) void k_muon_scale(NsArgs args, MuonTables t, f
   const MuonMat a = t.mats[c.mat0 + z];
   const MuonEntry e = t.entries[c.mat0 + z];
   const int tid = threadIdx.x;
-  double part = tid < a.blocks ? t.partials[(int64_t)(c.mat0 + z) * kMuonParts + tid] : 0.0;
+  double part = 0.0;
+  for (int i = tid; i < a.blocks; i += 256) part += t.partials[(int64_t)(c.mat0 + z) * kMuonParts + i];
   const double norm = sqrt(block_sum(part, lds)) + eps;
   const bool bad = !(norm < INFINITY);
   if (tl == 0 && tid == 0) t.info[c.mat0 + z] = bad ? 1 : 0;
@@ -187,16 +188,16 @@ __global__ __launch_bounds__(256) void k_muon_scale(NsArgs args, MuonTables t, f
         for (int i = 0; i < 8; ++i) b[i] = nesterov ? b[i] + mu * m[i] : m[i];
       }
     } else {
+      // single elements at clamped addresses, all in flight (behind a branch each they came one by one: 10 us for 201 x 327)
+      const int64_t rr = min(r, a.m - 1);
+      float m[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        b[i] = 0.f;
-        if (r < a.m && cc + i < a.n) {
-          b[i] = load_elem<GBF>(e.G, (int64_t)r * a.ldg + cc + i);
-          if (e.M) {
-            const float m = e.M[(int64_t)r * a.ldm + cc + i];
-            b[i] = nesterov ? b[i] + mu * m : m;
-          }
-        }
+      for (int i = 0; i < 8; ++i) b[i] = load_elem<GBF>(e.G, rr * a.ldg + min(cc + i, a.n - 1));
+      if (e.M) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m[i] = e.M[rr * a.ldm + min(cc + i, a.n - 1)];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = nesterov ? b[i] + mu * m[i] : m[i];
       }
     }
 #pragma unroll
@@ -806,8 +807,7 @@ OD_DEV void ns_final_tile(const NsJob& c, int z, int ti, int tj, const MuonTable
         if (whole) load8<XBF>(e.X, at, x);
         else {
 #pragma unroll
-          for (int q = 0; q < 8; ++q)
-            if (col + q < a.n) x[q] = load_elem<XBF>(e.X, at + q);
+          for (int q = 0; q < 8; ++q) x[q] = load_elem<XBF>(e.X, at + min(q, a.n - 1 - col));      // all in flight, no branch
         }
       }
 #pragma unroll
