@@ -521,7 +521,8 @@ __global__ __launch_bounds__(TL::THREADS, TL::blocks(PARTS)) void k_ns_products(
   const int64_t yplane = (int64_t)pp * c.lq, splane = (int64_t)c.p * c.lp;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   f32x16 acc[TL::FM][TL::FN];
-  if (c.kind == NS_APPLY) {
+  const int kind = __builtin_amdgcn_readfirstlane(c.kind);       // a scalar branch: the loads below set the lane mask
+  if (kind == NS_APPLY) {
     const int nj = (c.q + T - 1) / T;
     const int z = quotient(local, ni * nj), tl = local - z * (ni * nj);
     const int tj = quotient(tl, ni), ti = tl - tj * ni;
@@ -535,7 +536,7 @@ __global__ __launch_bounds__(TL::THREADS, TL::blocks(PARTS)) void k_ns_products(
       for (int e = 0; e < 4; ++e) x[e] = c.cc * acc[i][j][4 * v4 + e];
     }, slice + c.out, yplane, c.lq, row0, col0, c.p, qq, c.q, false);
   } else {
-    const bool full = c.kind == NS_FULL;
+    const bool full = kind == NS_FULL;
     const int splits = c.splits > 0 ? c.splits : 1, tiles = full ? ni * ni : ni * (ni + 1) / 2, per = tiles * splits;
     const int z = quotient(local, per), in_z = local - z * per, tile = quotient(in_z, splits), split = in_z - tile * splits;
     int ti, tj;
@@ -546,7 +547,7 @@ __global__ __launch_bounds__(TL::THREADS, TL::blocks(PARTS)) void k_ns_products(
       upper_tile(tile, ni, &ti, &tj);
     }
     uint16_t* slice = c.base + z * c.stride;
-    const bool gram = c.kind == NS_GRAM;
+    const bool gram = kind == NS_GRAM;
     const int64_t plane = gram ? yplane : splane;
     const int ld = gram ? c.lq : c.lp;
     const NsOperand A{slice + c.a + (int64_t)ti * T * ld, plane, ld, c.p - ti * T}, B{slice + c.b + (int64_t)tj * T * ld, plane, ld, c.p - tj * T};
@@ -841,7 +842,7 @@ __global__ __launch_bounds__(TL::THREADS, TL::blocks(PARTS)) void k_ns_final(NsA
   const int ni = (c.p + TL::T - 1) / TL::T, nj = (c.q + TL::T - 1) / TL::T, local = bid - c.first;
   const int z = quotient(local, ni * nj), tl = local - z * (ni * nj);
   const int tj = quotient(tl, ni), ti = tl - tj * ni;
-  if (c.tall) ns_final_tile<TL, PARTS, XBF, true>(c, z, ti, tj, t, update, keep, lr, lds);
+  if (__builtin_amdgcn_readfirstlane(c.tall)) ns_final_tile<TL, PARTS, XBF, true>(c, z, ti, tj, t, update, keep, lr, lds);
   else ns_final_tile<TL, PARTS, XBF, false>(c, z, ti, tj, t, update, keep, lr, lds);
 }
 
