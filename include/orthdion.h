@@ -304,8 +304,11 @@ int orthdion_step_static(orthdion_handle h, void* const* X, const void* const* G
  * pointers need the alignment of their type only.  Rows whose pointers and strides are multiples
  * of 16 bytes and 8 elements are moved faster.  A matrix is transposed on the way in where m > n.
  *
- * Arithmetic: accumulation is fp32, the norm fp64.  FAST: operands in fp16 under powers of two
- * (11 bits).  EXACT: two fp16 words per value, three products (22 bits).  AUTO as for orthdion_step.
+ * Arithmetic: B is formed in fp32, its norm in fp64; accumulation is fp32.  FAST: operands in fp16 under
+ * powers of two (11 bits; 22 in the orthogonalisation of small sets).  EXACT: two fp16 words per value,
+ * three products (22 bits).  AUTO as for orthdion_step.  Several steps may be evaluated as one polynomial
+ * of one S, where that loses no more than their rounding; which ones depends on shape, precision, the
+ * coefficients and the call.  Repeated calls on the same buffers give the same bits.
  * A zero matrix gives X_steps = 0.  A matrix with a NaN or an infinity in B gives NaN everywhere in
  * X (or O) and 1 in orthdion_muon_get_info; other matrices of the set are not affected.
  *
