@@ -529,6 +529,14 @@ def _per_item(name: str, value, count: int) -> List[float]:
     return got
 
 
+def _separate(name: str, written: List[int], read=()) -> None:
+    """Refuses a call that names one buffer twice among those that it writes, or reads one of them as another operand: workgroups would
+    race on it."""
+    once = set(written)
+    if len(once) != len(written) or not once.isdisjoint(read):
+        raise ValueError(f"{name}: one buffer is given twice, or for two operands (a tied parameter steps once; results need memory of their own)")
+
+
 class Muon:
     """Owns a handle and a torch-allocated workspace of the Muon step; tensors are the caller's.
 
@@ -603,17 +611,20 @@ class Muon:
         """One optimizer step: X and M are updated in place."""
         x, g = self._pointers("X", X, self._x_dtype, 0), self._pointers("G", G, self._g_dtype, 1)
         m = self._pointers("M", M, self._torch.float32, 2)
+        _separate("X, M", x + m, g)
         with _on_device(self._torch, self.workspace.get_device()):
             orthdion_muon_step(self.handle, x, g, m, self.workspace.data_ptr(), self.workspace_bytes, self._stream(stream))
 
     def orthogonalise(self, A, out, stream=None) -> None:
         """The orthogonalised A (laid out as G) into `out` (laid out as X)."""
         a, o = self._pointers("A", A, self._g_dtype, 1), self._pointers("out", out, self._x_dtype, 0)
+        _separate("out", o, a)
         with _on_device(self._torch, self.workspace.get_device()):
             orthdion_muon_orthogonalise(self.handle, a, o, self.workspace.data_ptr(), self.workspace_bytes, self._stream(stream))
 
     def info(self, stream=None) -> List[int]:
-        return orthdion_muon_get_info(self.handle, self.nmat, self._stream(stream))
+        with _on_device(self._torch, self.workspace.get_device()):
+            return orthdion_muon_get_info(self.handle, self.nmat, self._stream(stream))
 
     def set_lr(self, lr: float) -> None:
         orthdion_muon_set_lr(self.handle, lr)
@@ -668,6 +679,9 @@ class AdamW:
                         raise ValueError(f"{name}[{i}]: need a contiguous {dtype} tensor of {self.lengths[i]} elements on {counter.device}, "
                                          f"got {t.dtype} {tuple(t.shape)} on {t.device}, contiguous={t.is_contiguous()}")
             addresses.append(list(map(tensor.data_ptr, seq)))
+        x = addresses[0]
+        if len(set(x)) != len(x):
+            _separate("X", [a for a, n in zip(x, self.lengths) if n > 0])          # empty tensors have no memory
         with _on_device(torch, counter.get_device()):
             orthdion_adamw_step(self.handle, *addresses, counter.data_ptr(),
                                 stream if stream is not None else torch.cuda.current_stream(counter.device).cuda_stream)

@@ -266,7 +266,7 @@ template <int T>
 OD_DEV int swz_down(int k) { return T % 128 ? (k & 2) << 1 : (k & 3) << 2; }
 
 struct NsOperand {
-  const uint16_t* p;      // tile's first row (TRB: the tile's first column is in `edge`)
+  const uint16_t* p;      // tile's first row (TRB: column)
   int64_t plane;          // elements between parts
   int ld;
   int rows;               // rows (TRB: columns) from the tile's first one that may be read, at least 1 (TRB: 8)

@@ -338,3 +338,71 @@ def test_rows_beyond_32_bit_offsets():
     binding.Muon([(m, n)], x_dtype="f32").orthogonalise([g.float()], [o])
     host = g.double().cpu().numpy()
     check(o, newton_schulz(host, QUINTIC), tolerance(host, QUINTIC, True, "f32"))
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("shapes", [[(640, 1000), (640, 640), (96, 160), (1000, 640), (1, 9)], [(4 + 6 * i, 125 - 3 * i) for i in range(20)]])
+def test_sets_whose_members_are_planned_differently(shapes, x):
+    """Matrices with shared Gram matrices, step by step and small ones in the same launches; and more small shapes than a launch
+    takes.  Every matrix of the set is looked at, by itself and as a step."""
+    import torch
+    rng = np.random.default_rng(len(shapes))
+    dt = types(torch, x)
+    A = [upload(torch, matrix(rng, *s), dt)[1] for s in shapes]
+    O = [torch.empty_like(a) for a in A]
+    X = [torch.zeros(*s, device="cuda:0") for s in shapes]
+    M = [torch.zeros(*s, device="cuda:0") for s in shapes]
+    opt = binding.Muon(shapes, x_dtype=x)
+    opt.orthogonalise(A, O)
+    step = binding.Muon(shapes, x_dtype="f32", g_dtype=x, precision="fast" if x == "bf16" else "exact", mu=0.0, lr=-1.0, scale="none")
+    step.step(X, A, M)
+    assert opt.info() == step.info() == [0] * len(shapes)
+    for a, o, u in zip(A, O, X):
+        host = a.double().cpu().numpy()
+        want = newton_schulz(host, QUINTIC)
+        check(o, want, tolerance(host, QUINTIC, x == "f32", x))
+        check(u, want, 2 * tolerance(host, QUINTIC, x == "f32", "f32"))        # as in test_every_tile_and_plan
+
+
+def test_a_set_beyond_what_steps_together():
+    """More elements than share the workspace at a time: the later matrices take it over from the earlier ones.  Against handles
+    of their own; both lie within bf16's rounding and that of one-word operands of the same matrix."""
+    import torch
+    m, n, count = 40, 900000, 17
+    assert m * n * (count - 1) > 2 ** 29
+    gen = torch.Generator(device="cuda:0").manual_seed(9)
+    A = [torch.randn(m, n, device="cuda:0", generator=gen).bfloat16() for _ in range(count)]
+    O = [torch.empty_like(a) for a in A]
+    opt = binding.Muon([(m, n)] * count, x_dtype="bf16")
+    opt.orthogonalise(A, O)
+    assert opt.info() == [0] * count
+    alone = binding.Muon([(m, n)], x_dtype="bf16")
+    for k in (0, 14, 15, count - 1):
+        o = torch.empty_like(A[k])
+        alone.orthogonalise([A[k]], [o])
+        host = A[k].float().cpu().numpy().astype(np.float64)
+        s = np.sqrt(np.linalg.eigvalsh(host @ host.T))
+        # the same spectrum in a matrix small enough to iterate
+        tol = tolerance(np.diag(s), QUINTIC, False, "bf16")
+        assert float((O[k].float() - o.float()).norm() / o.float().norm()) <= 2 * tol, k
+
+
+def test_a_buffer_given_twice_is_refused():
+    import torch
+    opt = binding.Muon([(8, 8), (8, 8)], x_dtype="f32")
+    a, b, c, d, e, f = (torch.zeros(8, 8, device="cuda:0") for _ in range(6))
+    for call in (lambda: opt.step([a, a], [b, c], [d, e]), lambda: opt.step([a, b], [c, d], [e, e]), lambda: opt.step([a, b], [a, c], [d, e]),
+                 lambda: opt.step([a, b], [c, d], [a, e]), lambda: opt.orthogonalise([a, b], [c, c]), lambda: opt.orthogonalise([a, b], [a, c])):
+        with pytest.raises(ValueError):
+            call()
+    opt.orthogonalise([a, a], [b, c])
+    opt.step([a, b], [c, c], [d, e])
+    assert opt.info() == [0, 0]
+    counter = torch.zeros(2, dtype=torch.int32, device="cuda:0")
+    empty = torch.zeros(0, device="cuda:0")
+    adam = binding.AdamW([64, 64, 0, 0], x_dtype="f32")
+    rest = [b, c, empty, empty]
+    with pytest.raises(ValueError):
+        adam.step([a, a, empty, empty], rest, rest, rest, counter)
+    adam.step([a, b, empty, empty], [c, c, empty, empty], [d, e, empty, empty], [f, torch.zeros(8, 8, device="cuda:0"), empty, empty], counter)
+    assert counter.tolist() == [1, 0]
