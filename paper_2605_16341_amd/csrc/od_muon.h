@@ -42,7 +42,7 @@ enum NsKind : int {
   NS_APPLY = 2,                            // out = cc a b of p x p a and Y at b
   NS_FULL = 3,                             // out = cc a b of symmetric a, b, not mirrored
   NS_REDUCE = 4,                           // out = cc (sum of the partial sums at a)
-  NS_SMALL = 5                             // out = Z of a segment of steps from cc (sum of the partial sums at a)
+  NS_SMALL = 5                             // out = Z of a segment of steps from cc (sum of the partial sums at a; splits 0: a a^T of Y at a)
 };
 struct NsJob {
   int first;                               // first workgroup of the job
@@ -80,6 +80,10 @@ inline int64_t ns_partials(int p, int splits) {
 // Steps of a segment for the kernel that does all p x p work of a small matrix in LDS: coefficients and the powers of two
 // of the words of S, P, T = P S and Z that step k writes.
 constexpr int kNsSmall = 128;              // largest p
+inline int ns_small_size(int p) { return (p + 31) / 32 * 32; }
+// Whether that kernel computes the Gram matrix as well: Y then fits where the words of S and P will lie, 16 bytes a row for the
+// LDS banks included.  96 x 160 in two words: 82.4 us a call with launches of their own for the Gram matrices, 69.2 so.
+inline bool ns_small_whole(int p, int q, int parts) { return parts * ((q + kNsStep - 1) / kNsStep * kNsStep) <= 4 * ns_small_size(p); }
 constexpr int kNsMostSteps = 32;
 struct NsSteps {
   int count;

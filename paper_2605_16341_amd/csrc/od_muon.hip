@@ -642,7 +642,8 @@ __global__ __launch_bounds__(256) void k_ns_reduce(NsArgs args) {
   }
 }
 
-// All p x p work of a segment of steps for one matrix of p <= D, in one workgroup: S and P lie in LDS as two fp16 words a
+// All p x p work of a segment of steps for one matrix of p <= D, in one workgroup, with the Gram matrix before it where Y fits into
+// LDS: S and P lie in LDS as two fp16 words a
 // value (22 bits, three products), T = P S and Z in the accumulators' registers, from where they change places with S.
 // A wave has one 32 x 32 block.  A chain of products with a barrier after each: bound by the latency of LDS and barriers.
 template <int D>
@@ -694,10 +695,43 @@ __global__ __launch_bounds__(NsSmallTile<D>::THREADS, 1) void k_ns_small(NsJobs<
   };
   // S, zero outside the matrix
   f32x16 s, p, zz, t;
-  {
-    const float* in = reinterpret_cast<const float*>(slice + c.a) + row * kNsSplitTile + col0;
 #pragma unroll
-    for (int n = 0; n < 16; ++n) s[n] = 0.f;
+  for (int n = 0; n < 16; ++n) s[n] = 0.f;
+  if (c.splits == 0) {
+    // from Y, all of which fits where S and P will lie (ns_small_whole): at most eight 16-byte groups a thread, all in flight
+    const int qq = up64(c.q), slots = qq / 8, pitch = qq * 2 + 16, all = D * slots, most = PARTS * all;
+    const int64_t yplane = (int64_t)pp * c.lq;
+    const uint16_t* y = slice + c.a;
+    u32x4 w[8];
+    int at[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int n = min((int)threadIdx.x + i * TL::THREADS, most - 1), part = n >= all, r = (n - part * all) / slots, slot = n - part * all - r * slots;
+      w[i] = *reinterpret_cast<const u32x4*>(y + part * yplane + (int64_t)r * c.lq + slot * 8);
+      at[i] = (part * D + r) * pitch + slot * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<u32x4*>(lds + at[i]) = w[i];
+    __syncthreads();
+    f32x16 rest;
+#pragma unroll
+    for (int n = 0; n < 16; ++n) rest[n] = 0.f;
+    const char* pa = lds + row * pitch + (lane >> 5) * 16;
+    const char* pb = lds + (block + (lane & 31)) * pitch + (lane >> 5) * 16;
+#pragma unroll 4
+    for (int ks = 0; ks < qq / 16; ++ks) {
+      const u32x4 ah = *reinterpret_cast<const u32x4*>(pa + 32 * ks), bh = *reinterpret_cast<const u32x4*>(pb + 32 * ks);
+      s = mfma_32x32x16<true>(bh, ah, s);
+      if constexpr (PARTS == 2) {
+        const u32x4 al = *reinterpret_cast<const u32x4*>(pa + D * pitch + 32 * ks), bl = *reinterpret_cast<const u32x4*>(pb + D * pitch + 32 * ks);
+        rest = mfma_32x32x16<true>(bl, ah, rest);
+        rest = mfma_32x32x16<true>(bh, al, rest);
+      }
+    }
+    s += rest;
+    __syncthreads();
+  } else {
+    const float* in = reinterpret_cast<const float*>(slice + c.a) + row * kNsSplitTile + col0;
 #pragma unroll 4
     for (int split = 0; split < c.splits; ++split)
 #pragma unroll
@@ -706,9 +740,9 @@ __global__ __launch_bounds__(NsSmallTile<D>::THREADS, 1) void k_ns_small(NsJobs<
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[4 * v4 + e] += x[e];
       }
-#pragma unroll
-    for (int n = 0; n < 16; ++n) s[n] = row < c.p && col0 + 8 * (n >> 2) + (n & 3) < c.p ? c.cc * s[n] : 0.f;
   }
+#pragma unroll
+  for (int n = 0; n < 16; ++n) s[n] = row < c.p && col0 + 8 * (n >> 2) + (n & 3) < c.p ? c.cc * s[n] : 0.f;
   for (int l = 0; l < k.count; ++l) {
     if (l > 0) {
       t = product(p_plane, s_plane) * (1.f / (k.p[l - 1] * k.s[l - 1]));            // T = P S
@@ -1002,7 +1036,7 @@ namespace {
 
 template <int D, int PARTS>
 hipError_t small_of(const NsArgs& a, const NsSteps& steps, hipStream_t st) {
-  const NsJobs<kNsClasses> o = laid_out<kNsClasses>(a, [](const NsJob& c) { return (c.p + 31) / 32 * 32 == D; }, [](const NsJob&) { return 1; });
+  const NsJobs<kNsClasses> o = laid_out<kNsClasses>(a, [](const NsJob& c) { return ns_small_size(c.p) == D; }, [](const NsJob&) { return 1; });
   return go<NsSmallTile<D>, PARTS>(k_ns_small<D, PARTS>, o, st, steps);
 }
 

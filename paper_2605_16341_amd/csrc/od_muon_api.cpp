@@ -91,11 +91,12 @@ Mode mode_for(int p, int q) {
 // word O of 400 x 600 is 1.95e-3 off before bf16's 1.7e-3.  The step, whose X takes lr O, keeps one.
 constexpr int64_t kTwoWordWork = (int64_t)1 << 29;
 
-// Splits of the K range of a class's Gram matrices.  For the kernel that adds them up by itself (SMALL): its workgroup
-// reads 64 KB a split, about as long as two steps take, so the square root of the steps balances the two.  Otherwise
+// Splits of the K range of a class's Gram matrices, 0: one sum.  For the kernel that adds them up by itself (SMALL), unless it
+// computes them as well: its workgroup reads 64 KB a split, about as long as two steps take, so the square root of the steps balances the two.  Otherwise
 // where the tiles leave most of the chip idle and the range is long: one round of workgroups, at least eight steps each.
-int splits_for(Mode mode, int p, int q, int nb) {
+int splits_for(Mode mode, int p, int q, int nb, int parts) {
   const int64_t steps = up64(q) / od::kNsStep;
+  if (mode == SMALL && od::ns_small_whole(p, q, parts)) return 0;
   if (mode == SMALL) return (int)std::min<int64_t>(64, std::max<int64_t>(1, (int64_t)std::lround(std::sqrt(0.6 * (double)steps))));
   const int64_t n = (p + od::kNsSplitTile - 1) / od::kNsSplitTile, tiles = n * (n + 1) / 2 * nb;
   if (tiles >= 128 || steps < 16) return 0;
@@ -212,8 +213,10 @@ static void plan_jobs(const std::vector<Step>& steps, Mode mode, bool split, int
         list.t[l] = two(exponent_for(st.poly * st.top * st.top));
         list.z[l] = two(exponent_for(product_bound(steps, k, l + 1)));
       }
-      plan->stages.push_back({PlannedJob{od::NS_GRAM, {IN_Y, src}, {IN_Y, src}, none, partials, 0.f, 0.f, 1.f}});
-      plan->stages.push_back({PlannedJob{od::NS_SMALL, partials, none, none, s_mat, 0.f, 0.f, two(-2 * exp_y)}});
+      const Operand y{IN_Y, src};
+      plan->stages.push_back({});          // the same number of stages with and without
+      if (split) plan->stages.back().push_back(PlannedJob{od::NS_GRAM, y, y, none, partials, 0.f, 0.f, 1.f});
+      plan->stages.push_back({PlannedJob{od::NS_SMALL, split ? partials : y, none, none, s_mat, 0.f, 0.f, two(-2 * exp_y)}});
       plan->steps.push_back(list);
       apply_of(s_mat, exponent_for(product_bound(steps, k, length)));
       continue;
@@ -330,7 +333,7 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
     // 209 us a step, with launches of their own kernel in between 275.
     Mode mode = mode_for(c.p, c.q);
     if (mode == SMALL && !all_small) mode = STEP_BY_STEP;
-    const int splits = splits_for(mode, c.p, c.q, (int)c.members.size());
+    const int splits = splits_for(mode, c.p, c.q, (int)c.members.size(), h->parts[0]);
     const Plan* const plan[2] = {&h->plans[0][splits > 0][mode], &h->plans[1][splits > 0][mode]};
     const int symmetric = std::max(plan[0]->symmetric, plan[1]->symmetric);
     const int64_t stride = h->parts[0] * (2 * od::ns_y_plane(c.p, lq) + symmetric * od::ns_s_plane(c.p, lp)) + od::ns_partials(c.p, splits);

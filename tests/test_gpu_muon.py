@@ -406,3 +406,20 @@ def test_a_buffer_given_twice_is_refused():
         adam.step([a, a, empty, empty], rest, rest, rest, counter)
     adam.step([a, b, empty, empty], [c, c, empty, empty], [d, e, empty, empty], [f, torch.zeros(8, 8, device="cuda:0"), empty, empty], counter)
     assert counter.tolist() == [1, 0]
+
+
+@pytest.mark.parametrize("shape", [(30, 64), (30, 65), (30, 128), (129, 30), (33, 128), (64, 129), (256, 64), (64, 257), (96, 192), (193, 96), (90, 384),
+                                   (90, 385), (128, 256), (128, 257), (512, 128), (127, 513)])
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+def test_small_matrices_around_the_ends_of_one_workgroup(shape, x):
+    """Gram matrices that the kernel for small matrices computes by itself, and those just too long for it; three of each."""
+    import torch
+    rng = np.random.default_rng(shape[0] + shape[1])
+    A = [upload(torch, matrix(rng, *shape, kind), types(torch, x))[1] for kind in ("noise", "spiked", "noise")]
+    O = [torch.empty_like(a) for a in A]
+    opt = binding.Muon([shape] * 3, x_dtype=x)
+    opt.orthogonalise(A, O)
+    assert opt.info() == [0] * 3
+    for a, o in zip(A, O):
+        host = a.double().cpu().numpy()
+        check(o, newton_schulz(host, QUINTIC), tolerance(host, QUINTIC, x == "f32", x))
