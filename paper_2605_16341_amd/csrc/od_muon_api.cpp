@@ -70,7 +70,8 @@ struct Cluster {
 // max |P|^2 would pass a limit.  Emulated on matrices of power-law, spiked and flat spectra, relative error of O for the published
 // coefficients:
 //   one fp16 word, 512 x 1024 to 1528 x 3304: step by step 0.9 to 3.0e-3, cut 2 + 2 + 1 1.2 to 2.4e-3, 3 + 2 0.9 to 2.7e-3,
-//   2 + 3 up to 9e-3, in one segment up to 0.5
+//   2 + 3 up to 9e-3, in one segment up to 0.5; measured on 136 x 4096 to 500 x 2000, flat, spiked, 1 / n and 1 / n^2 spectra: step by
+//   step 1.1 to 3.8e-3 (1 / n^2 2.0e-2), 2 + 2 + 1 1.1 to 3.3e-3 (1.9e-2), 3 + 2 1.5 to 4.3e-3 (2.0e-2)
 //   two words, 40 x 200 to 512 x 2048: step by step 1.1 to 6.1e-6, 2 + 1 + 2 1.1 to 5.2e-6, 2 + 2 + 1 1.2 to 5.2e-6 (twice as
 //   much as step by step on some), 3 + 2 1.1 to 7e-6
 //   one word for Y, two for the p x p work (small matrices), 40 x 200 to 300 x 700: 3 + 2 0.5 to 1.4e-3, in one segment 0.3 to 5.4e-3
@@ -79,11 +80,14 @@ constexpr double kGrowth = 13.0, kLongGrowth = 160.0;
 // fast precision, whose X of 8 bits takes lr O (24 decoder layers: 40.8 -> 35.6 ms), and by small matrices.
 bool long_first(Mode mode, int parts, bool step) { return parts == 1 && (mode == SMALL || step); }
 // In units of p^3 a step by itself costs 3 rho + 1 with rho = q / p, a segment of L steps 3 rho + 4 L - 3: the same for two
-// segments of 3 + 2 and five steps at rho = 1.  But a segment has more and smaller launches.
-constexpr int kSegmentRows = 512;
+// segments of 3 + 2 and five steps at rho = 1.  But a segment has more and smaller launches, so matrices of few rows need long
+// ones (us, orthogonalisation step by step / in segments): bf16 136 x 1024 150 / 137, 136 x 16384 206 / 175, 16 of 256 x 1024 156 / 140, of
+// 256 x 768 108 / 113, of 384 x 1152 202 / 187, 8 of 480 x 1440 203 / 188, of 480 x 960 154 / 160; fp32 16 of 256 x 1024 215 / 189.
+constexpr int kSegmentRows = 512, kSegmentColumns = 1024;
 Mode mode_for(int p, int q) {
   if (p <= od::kNsSmall) return SMALL;
-  return p >= kSegmentRows && 4 * (int64_t)q >= 5 * (int64_t)p ? SEGMENTS : STEP_BY_STEP;
+  const bool segments = p >= kSegmentRows ? 4 * (int64_t)q >= 5 * (int64_t)p : q >= kSegmentColumns && q >= 3 * (int64_t)p;
+  return segments ? SEGMENTS : STEP_BY_STEP;
 }
 
 // In fast precision the orthogonalisation takes two words where that costs next to nothing, in sets so small that launches
