@@ -81,8 +81,8 @@ constexpr double kGrowth = 13.0, kLongGrowth = 160.0;
 bool long_first(Mode mode, int parts, bool step) { return parts == 1 && (mode == SMALL || step); }
 // In units of p^3 a step by itself costs 3 rho + 1 with rho = q / p, a segment of L steps 3 rho + 4 L - 3: the same for two
 // segments of 3 + 2 and five steps at rho = 1.  But a segment has more and smaller launches, so matrices of few rows need long
-// ones (us, orthogonalisation step by step / in segments): bf16 136 x 1024 150 / 137, 136 x 16384 206 / 175, 16 of 256 x 1024 156 / 140, of
-// 256 x 768 108 / 113, of 384 x 1152 202 / 187, 8 of 480 x 1440 203 / 188, of 480 x 960 154 / 160; fp32 16 of 256 x 1024 215 / 189.
+// ones (us a step, step by step / in segments): bf16 136 x 1024 112 / 104, 136 x 16384 158 / 125, 16 of 256 x 1024 157 / 134, of 256 x 768
+// 113 / 119, of 384 x 1152 209 / 193, 8 of 480 x 1440 213 / 193, of 480 x 960 154 / 168; fp32 16 of 256 x 1024 217 / 192.
 constexpr int kSegmentRows = 512, kSegmentColumns = 1024;
 Mode mode_for(int p, int q) {
   if (p <= od::kNsSmall) return SMALL;
@@ -95,16 +95,26 @@ Mode mode_for(int p, int q) {
 // word O of 400 x 600 is 1.95e-3 off before bf16's 1.7e-3.  The step, whose X takes lr O, keeps one.
 constexpr int64_t kTwoWordWork = (int64_t)1 << 29;
 
+int64_t gram_tiles(int p, int64_t nb) {
+  const int64_t n = (p + od::kNsSplitTile - 1) / od::kNsSplitTile;
+  return n * (n + 1) / 2 * nb;
+}
+
 // Splits of the K range of a class's Gram matrices, 0: one sum.  For the kernel that adds them up by itself (SMALL), unless it
-// computes them as well: its workgroup reads 64 KB a split, about as long as two steps take, so the square root of the steps balances the two.  Otherwise
-// where the tiles leave most of the chip idle and the range is long: one round of workgroups, at least eight steps each.
-int splits_for(Mode mode, int p, int q, int nb, int parts) {
+// computes them as well: its workgroup reads 64 KB a split, about as long as two steps take, so the square root of the steps
+// balances the two.  Otherwise where the tiles leave most of the chip idle and the range is long: at most one round of workgroups,
+// and as many splits as balance a workgroup's steps with the adding up, whose time grows with the splits and with the tiles of the
+// set (`beside`).  Against eight steps a split (us, orthogonalisation, fp32): 200 x 4096 152 -> 144, 150 x 1024 139 -> 124, 4 of 200 x 1500
+// 166 -> 156, 130 x 60000 316 -> 275, 4 of 512 x 4096 337 -> 301, 20 of 136 x 4096 334 -> 296, 480 x 9000 246 -> 248.
+int splits_for(Mode mode, int p, int q, int nb, int64_t beside, int parts) {
   const int64_t steps = up64(q) / od::kNsStep;
   if (mode == SMALL && od::ns_small_whole(p, q, parts)) return 0;
   if (mode == SMALL) return (int)std::min<int64_t>(64, std::max<int64_t>(1, (int64_t)std::lround(std::sqrt(0.6 * (double)steps))));
-  const int64_t n = (p + od::kNsSplitTile - 1) / od::kNsSplitTile, tiles = n * (n + 1) / 2 * nb;
+  const int64_t tiles = gram_tiles(p, nb);
   if (tiles >= 128 || steps < 16) return 0;
-  return (int)std::min<int64_t>((256 + tiles - 1) / tiles, steps / 8);
+  const int64_t depth = std::max(1L, std::lround(std::sqrt((double)steps * (double)(16 + beside) / 80.0)));       // steps of a split
+  const int64_t splits = std::min<int64_t>(256 / tiles, (steps + depth - 1) / depth);
+  return splits > 1 ? (int)splits : 0;
 }
 
 // power of two that brings values up to `bound` to 2^13 at most, three bits below the end of fp16's range
@@ -319,6 +329,12 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
     classes[k].members.push_back(i);
   }
   bool all_small = true;
+  // Beside larger matrices small ones ride along in their launches, which are there anyway: six matrices of 128 to 392 rows
+  // 209 us a step, with launches of their own kernel in between 275.
+  auto mode_of = [&](const Shape& c) {
+    const Mode mode = mode_for(c.p, c.q);
+    return mode == SMALL && !all_small ? STEP_BY_STEP : mode;
+  };
   for (const Shape& c : classes) all_small = all_small && mode_for(c.p, c.q) == SMALL;
   double work = 0.0;
   for (const Shape& c : classes) work += (double)c.p * c.p * c.q * (double)c.members.size();
@@ -327,18 +343,29 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
   for (int step = 0; step < 2; ++step)
     for (int split = 0; split < 2; ++split)
       for (int mode = 0; mode < kModes; ++mode) plan_jobs(steps, (Mode)mode, split != 0, h->parts[step], step != 0, &h->plans[step][split][mode]);
+  // Splits; where those of the set would take more than two workgroups a CU, fewer of each (a 1024-wide model in fp32, 576 workgroups
+  // 791 us a step, 432 688)
+  int64_t beside = 0, groups = 0;
+  for (const Shape& c : classes) beside += gram_tiles(c.p, (int64_t)c.members.size());
+  std::vector<int> splits_of;
+  for (const Shape& c : classes) {
+    splits_of.push_back(splits_for(mode_of(c), c.p, c.q, (int)c.members.size(), beside, h->parts[0]));
+    groups += gram_tiles(c.p, (int64_t)c.members.size()) * splits_of.back();
+  }
+  if (!all_small && groups > 512)
+    for (int& splits : splits_of) splits = (int)(splits * (int64_t)512 / groups) > 1 ? (int)(splits * (int64_t)512 / groups) : 0;
   // clusters
   int64_t held = 0;
   size_t slices = 0, most = 0;
   for (const Shape& c : classes) {
     const int64_t elements = (int64_t)c.p * c.q;
     const int lp = pitch(c.p), lq = pitch(c.q);
-    // Beside larger matrices small ones ride along in their launches, which are there anyway: six matrices of 128 to 392 rows
-    // 209 us a step, with launches of their own kernel in between 275.
-    Mode mode = mode_for(c.p, c.q);
-    if (mode == SMALL && !all_small) mode = STEP_BY_STEP;
-    const int splits = splits_for(mode, c.p, c.q, (int)c.members.size(), h->parts[0]);
-    const Plan* const plan[2] = {&h->plans[0][splits > 0][mode], &h->plans[1][splits > 0][mode]};
+    const Mode mode = mode_of(c);
+    // O in one word of few rows: 2 + 2 + 1 steps left 2.6 to 3.4e-3 on 136 x 16384 of a falling spectrum, step by step 2.2e-3 (bf16's rounding
+    // alone 1.7e-3)
+    const Mode alone = mode == SEGMENTS && c.p < kSegmentRows && h->parts[0] == 1 ? STEP_BY_STEP : mode;
+    const int splits = splits_of[&c - classes.data()];
+    const Plan* const plan[2] = {&h->plans[0][splits > 0][alone], &h->plans[1][splits > 0][mode]};
     const int symmetric = std::max(plan[0]->symmetric, plan[1]->symmetric);
     const int64_t stride = h->parts[0] * (2 * od::ns_y_plane(c.p, lq) + symmetric * od::ns_s_plane(c.p, lp)) + od::ns_partials(c.p, splits);
     for (size_t done = 0; done < c.members.size();) {
