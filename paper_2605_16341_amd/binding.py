@@ -231,8 +231,12 @@ def orthdion_set_variant(handle: int, variant: int) -> None:
     _check(load().orthdion_set_variant(handle, int(variant)))
 
 
-def _ptr_array(ptrs: Sequence[int]):
-    return (ctypes.c_void_p * len(ptrs)).from_buffer(array.array("Q", ptrs)) if ptrs else (ctypes.c_void_p * 0)()
+def _ptr_array(ptrs: Sequence[Optional[int]]):
+    """Host array of device addresses; None is a null pointer."""
+    try:
+        return (ctypes.c_void_p * len(ptrs)).from_buffer(array.array("Q", ptrs)) if len(ptrs) else (ctypes.c_void_p * 0)()
+    except (TypeError, OverflowError):         # what else ctypes takes for an address: None, c_void_p, an address as a signed number
+        return (ctypes.c_void_p * len(ptrs))(*ptrs)
 
 
 def orthdion_step(handle: int, X: Sequence[int], G: Sequence[int], M: Sequence[int], Q: Sequence[int],

@@ -1,0 +1,44 @@
+"""CPU-only checks of the binding's own handling of arguments, before anything reaches the library."""
+import ctypes
+
+import pytest
+
+from paper_2605_16341_amd import binding as b
+
+FAKE = 1 << 20            # an aligned "device address", never dereferenced
+
+
+def status_of(call):
+    with pytest.raises(b.OrthDionError) as e:
+        call()
+    return e.value.status
+
+
+@pytest.mark.parametrize("ptrs,want", [([], []), ([FAKE], [FAKE]), ([FAKE, 2 ** 64 - 8], [FAKE, 2 ** 64 - 8]), ([None, FAKE], [None, FAKE]),
+                                       ([ctypes.c_void_p(FAKE), FAKE], [FAKE, FAKE]), ([-8, 0], [2 ** 64 - 8, None]), ((FAKE, None), [FAKE, None])])
+def test_addresses(ptrs, want):
+    assert list(b._ptr_array(ptrs)) == want
+
+
+def test_null_addresses_reach_the_library():
+    """None stands for a null pointer: refused by the library where there is something behind it, taken for an empty tensor."""
+    h = b.orthdion_create([(64, 64)], 8, b.ORTHDION_F32, b.ORTHDION_F32)
+    need = b.orthdion_workspace_bytes(h)
+    for k in range(4):
+        ptrs = [[None] if i == k else [FAKE] for i in range(4)]
+        assert status_of(lambda: b.orthdion_step(h, *ptrs, FAKE, need)) == b.ORTHDION_E_NULL_PTR
+    b.orthdion_destroy(h)
+    h = b.orthdion_muon_create([(64, 64)], b.ORTHDION_F32, b.ORTHDION_F32)
+    assert status_of(lambda: b.orthdion_muon_step(h, [None], [FAKE], [FAKE], FAKE, b.orthdion_muon_workspace_bytes(h))) == b.ORTHDION_E_NULL_PTR
+    b.orthdion_muon_destroy(h)
+    h = b.orthdion_adamw_create([5, 0], b.ORTHDION_F32, b.ORTHDION_F32)
+    some, odd = [FAKE, None], [FAKE + 2, None]
+    assert status_of(lambda: b.orthdion_adamw_step(h, [None, None], some, some, some, FAKE)) == b.ORTHDION_E_NULL_PTR
+    assert status_of(lambda: b.orthdion_adamw_step(h, some, odd, some, some, FAKE)) == b.ORTHDION_E_MISALIGNED      # not the empty one's null
+    b.orthdion_adamw_destroy(h)
+
+
+@pytest.mark.parametrize("ptrs", [["8"], [1.5], [object()]])
+def test_what_is_no_address_is_refused(ptrs):
+    with pytest.raises(TypeError):
+        b._ptr_array(ptrs)
