@@ -665,6 +665,14 @@ class AdamW:
         self.handle = orthdion_adamw_create(self.lengths, xc, gc, lr, betas[0], betas[1], eps,
                                             _per_item("weight_decay", weight_decay, count), _per_item("lr_scale", lr_scale, count))
 
+    def _separate_tensors(self, x, g, m, v) -> None:
+        """Refuses one buffer for two of the tensors that the step writes, or for one of them and a gradient."""
+        written = x + m + v
+        once = set(written)
+        if len(once) != len(written) or not once.isdisjoint(g):
+            held = [[a for a, n in zip(seq, self.lengths) if n > 0] for seq in (x, m, v, g)]       # empty tensors have no memory
+            _separate("X, M, V", held[0] + held[1] + held[2], held[3])
+
     def step(self, X, G, M, V, counter, stream=None) -> None:
         """One step: X, M and V are updated in place.  `counter` is an int32 tensor of two on the tensors' device, [steps taken
         so far, 0]; the step advances it there."""
@@ -683,9 +691,7 @@ class AdamW:
                         raise ValueError(f"{name}[{i}]: need a contiguous {dtype} tensor of {self.lengths[i]} elements on {counter.device}, "
                                          f"got {t.dtype} {tuple(t.shape)} on {t.device}, contiguous={t.is_contiguous()}")
             addresses.append(list(map(tensor.data_ptr, seq)))
-        x = addresses[0]
-        if len(set(x)) != len(x):
-            _separate("X", [a for a, n in zip(x, self.lengths) if n > 0])          # empty tensors have no memory
+        self._separate_tensors(*addresses)
         with _on_device(torch, counter.get_device()):
             orthdion_adamw_step(self.handle, *addresses, counter.data_ptr(),
                                 stream if stream is not None else torch.cuda.current_stream(counter.device).cuda_stream)

@@ -42,3 +42,22 @@ def test_null_addresses_reach_the_library():
 def test_what_is_no_address_is_refused(ptrs):
     with pytest.raises(TypeError):
         b._ptr_array(ptrs)
+
+
+def test_adamw_refuses_a_buffer_given_twice():
+    """Addresses of the four lists of a step over tensors of 4, 6 and 0 elements; the empty one's may be any."""
+    opt = b.AdamW([4, 6, 0], x_dtype="f32")
+    good = [[64, 128, 0], [192, 256, 0], [320, 384, 0], [448, 512, 0]]          # X, G, M, V
+    opt._separate_tensors(*good)
+    opt._separate_tensors(good[0], [192, 192, 64], good[2], good[3])           # gradients are only read
+    for written in (0, 2, 3):
+        twice = [list(seq) for seq in good]
+        twice[written][1] = twice[written][0]
+        with pytest.raises(ValueError):
+            opt._separate_tensors(*twice)
+        for other in (0, 1, 2, 3):
+            if other != written:
+                shared = [list(seq) for seq in good]
+                shared[other][0] = shared[written][1]
+                with pytest.raises(ValueError):
+                    opt._separate_tensors(*shared)
