@@ -58,9 +58,9 @@ struct AdamCoef {
 OD_DEV float adam_one(float x, float g, float& m, float& v, const AdamCoef& k) {
   m = k.b1 * m + k.a1 * g;
   v = k.b2 * v + k.a2 * (g * g);
-  // square root and reciprocal to one unit in the last place
-  const float d = __builtin_amdgcn_sqrtf(v * k.c2) + k.eps;
-  return k.keep * x - k.step * (m * k.c1 * __builtin_amdgcn_rcpf(d));
+  // rounded square root and quotient: the hardware's own take v or d below 2^-126 for zero, which with eps = 0 moved x to infinity
+  const float d = __builtin_sqrtf(v * k.c2) + k.eps;
+  return k.keep * x - k.step * (m * k.c1 / d);
 }
 
 template <bool XBF, bool GBF>

@@ -1,6 +1,10 @@
 """Muon and AdamW on the GPU where a call or its values lie at the edge of what is accepted."""
+import math
+
+import numpy as np
 import pytest
 
+from oracle.optimizers_oracle import adamw_step
 from paper_2605_16341_amd import binding
 
 pytestmark = pytest.mark.gpu
@@ -21,3 +25,32 @@ def test_adamw_refuses_a_buffer_given_twice_and_leaves_the_state():
     assert counter.tolist() == [0, 0] and all(bool((t == k).all()) for k, t in enumerate((a, b, c, d, e, f, g, h), 1))
     call((a, b), (c, c), (d, e), (f, g))
     assert counter.tolist() == [1, 0]
+
+
+def adamw_once(g, eps, lr=0.25, beta1=0.9, beta2=0.95, t0=0, x0=0.0, m0=0.0, v0=0.0):
+    """x, m, v after a step of fp32 tensors in fp64, and what the oracle says of them; the scalars are those that fp32 holds."""
+    import torch
+    f = lambda a: torch.as_tensor(a, dtype=torch.float32, device="cuda:0").expand(len(g)).contiguous()
+    opt = binding.AdamW([len(g)], x_dtype="f32", lr=lr, betas=(beta1, beta2), eps=eps)
+    x, grad, m, v = f(x0), f(g), f(m0), f(v0)
+    before = [a.double().cpu().numpy() for a in (x, grad, m, v)]
+    opt.step([x], [grad], [m], [v], torch.tensor([t0, 0], dtype=torch.int32, device="cuda:0"))
+    return [a.double().cpu().numpy() for a in (x, m, v)], adamw_step(*before, t0 + 1, lr, beta1, beta2, float(np.float32(eps)), 0.0)
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-45, 1e-40, 1e-30, 1e-8])
+def test_adamw_of_tiny_gradients(eps):
+    """Second moments below the smallest normal number are held in steps of 2^-149: half a step and the gradient's 2^-24 off, and
+    with eps = 0 the step is their root's."""
+    g = [s * a for a in (1e-16, 1e-18, 1e-19, 3e-20, 1e-20) for s in (1.0, -1.0)]
+    (x, m, v), (wx, wm, wv) = adamw_once(g, eps)
+    assert np.all(np.abs(v - wv) <= 2.0 ** -149 + 6 * 2.0 ** -24 * wv)
+    # v off by a share e leaves its root e / 2 off; v is corrected in fp32 too, a multiple of 2^-149 again
+    share = 2 * (2.0 ** -149 / wv) + 16 * 2.0 ** -24
+    assert np.all(np.abs(x - wx) <= share * np.abs(wx)), (x, wx)
+
+
+@pytest.mark.parametrize("eps", [1e-45, 1e-40, 1e-8])
+def test_adamw_without_gradients_stays_with_any_eps(eps):
+    (x, m, v), _ = adamw_once([0.0] * 9, eps, x0=0.5)
+    assert np.all(x == 0.5) and np.all(m == 0) and np.all(v == 0)
