@@ -51,15 +51,16 @@ OD_DEV double power(double x, int n) {
   return r;
 }
 
-struct AdamCoef {
+struct AdamCoef {                          // c1 and c2: 1 / (1 - b1^t) and the root of 1 / (1 - b2^t)
   float b1, a1, b2, a2, c1, c2, eps, keep, step;
 };
 
 OD_DEV float adam_one(float x, float g, float& m, float& v, const AdamCoef& k) {
   m = k.b1 * m + k.a1 * g;
-  v = k.b2 * v + k.a2 * (g * g);
+  // factor by factor, so that only a v out of range overflows: g^2 does from 1.8e19 on, v / (1 - b2^t) is g^2 at first
+  v = k.b2 * v + k.a2 * g * g;
   // rounded square root and quotient: the hardware's own take v or d below 2^-126 for zero, which with eps = 0 moved x to infinity
-  const float d = __builtin_sqrtf(v * k.c2) + k.eps;
+  const float d = __builtin_sqrtf(v) * k.c2 + k.eps;
   return k.keep * x - k.step * (m * k.c1 / d);
 }
 
@@ -75,7 +76,7 @@ __global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamArgs a) {
   const AdamTensor& t = a.t[lo];
   const int steps = a.counter[0] + 1;
   const AdamCoef k{(float)a.beta1, (float)(1.0 - a.beta1), (float)a.beta2, (float)(1.0 - a.beta2),
-                   (float)(1.0 / (1.0 - power(a.beta1, steps))), (float)(1.0 / (1.0 - power(a.beta2, steps))), a.eps, t.keep, t.step};
+                   (float)(1.0 / (1.0 - power(a.beta1, steps))), (float)sqrt(1.0 / (1.0 - power(a.beta2, steps))), a.eps, t.keep, t.step};
   const int64_t begin = (int64_t)(bid - t.first) * kAdamSpan, end = min(t.n, begin + kAdamSpan);
   uint16_t* xh = reinterpret_cast<uint16_t*>(t.X);
   float* xf = reinterpret_cast<float*>(t.X);

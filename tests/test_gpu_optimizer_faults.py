@@ -54,3 +54,15 @@ def test_adamw_of_tiny_gradients(eps):
 def test_adamw_without_gradients_stays_with_any_eps(eps):
     (x, m, v), _ = adamw_once([0.0] * 9, eps, x0=0.5)
     assert np.all(x == 0.5) and np.all(m == 0) and np.all(v == 0)
+
+
+@pytest.mark.parametrize("beta2", [0.95, 0.999])
+@pytest.mark.parametrize("t0", [0, 5])
+def test_adamw_of_huge_gradients(beta2, t0):
+    """Second moments within fp32 whose gradient's square or bias-corrected value lies beyond it."""
+    g = [s * a for a in (1e15, 2e19, 5e19) for s in (1.0, -1.0)]
+    (x, m, v), (wx, wm, wv) = adamw_once(g, 1e-8, beta2=beta2, t0=t0)
+    assert wv.max() < 3e38 < 2.5e39 <= max(g) ** 2
+    # four roundings a moment, and of x those of the root, its factor, the sum, the quotient and the products: 16 halves of a step
+    assert np.all(np.abs(v - wv) <= 6 * 2.0 ** -24 * wv) and np.all(np.abs(m - wm) <= 4 * 2.0 ** -24 * np.abs(wm))
+    assert np.all(np.abs(x - wx) <= 16 * 2.0 ** -24 * np.abs(wx)), (x, wx)
