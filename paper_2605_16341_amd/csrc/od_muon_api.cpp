@@ -76,9 +76,9 @@ struct Cluster {
 //   much as step by step on some), 3 + 2 1.1 to 7e-6
 //   one word for Y, two for the p x p work (small matrices), 40 x 200 to 300 x 700: 3 + 2 0.5 to 1.4e-3, in one segment 0.3 to 5.4e-3
 constexpr double kGrowth = 13.0, kLongGrowth = 160.0;
-// The long first segment (3 + 2) is taken where O does not leave by itself with the precision of one word: by the step in
-// fast precision, whose X of 8 bits takes lr O (24 decoder layers: 40.8 -> 35.6 ms), and by small matrices.
-bool long_first(Mode mode, int parts, bool step) { return parts == 1 && (mode == SMALL || step); }
+// The long first segment (3 + 2) is taken where O does not leave with the precision of one word: by the step of a bf16 X in
+// fast precision, whose 8 bits take lr O (24 decoder layers: 40.8 -> 35.6 ms; `coarse`), and by small matrices.
+bool long_first(Mode mode, int parts, bool coarse) { return parts == 1 && (mode == SMALL || coarse); }
 // In units of p^3 a step by itself costs 3 rho + 1 with rho = q / p, a segment of L steps 3 rho + 4 L - 3: the same for two
 // segments of 3 + 2 and five steps at rho = 1.  But a segment has more and smaller launches, so matrices of few rows need long
 // ones (us a step, step by step / in segments): bf16 136 x 1024 112 / 104, 136 x 16384 158 / 125, 16 of 256 x 1024 157 / 134, of 256 x 768
@@ -189,7 +189,7 @@ static double product_bound(const std::vector<Step>& steps, int from, int count)
   return std::max(1.02 * most, 1.0 / 256);
 }
 
-static void plan_jobs(const std::vector<Step>& steps, Mode mode, bool split, int parts, bool step, Plan* plan) {
+static void plan_jobs(const std::vector<Step>& steps, Mode mode, bool split, int parts, bool coarse, Plan* plan) {
   const int count = (int)steps.size() - 1;
   const Operand none{IN_SYMMETRIC, 0}, s_mat{IN_SYMMETRIC, 0}, t_mat{IN_SYMMETRIC, 1}, partials{IN_PARTIALS, 0};
   auto two = [](int e) { return (float)std::ldexp(1.0, e); };
@@ -199,7 +199,7 @@ static void plan_jobs(const std::vector<Step>& steps, Mode mode, bool split, int
     int length = 1;
     // two words: only the first and the last segment hold more than one step
     if (mode != STEP_BY_STEP && (parts == 1 || k == 0 || k + 2 == count)) {
-      const double limit = k == 0 && long_first(mode, parts, step) ? kLongGrowth : kGrowth;
+      const double limit = k == 0 && long_first(mode, parts, coarse) ? kLongGrowth : kGrowth;
       double growth = 1.0;
       while (k + length < count) {
         growth *= steps[k + length - 1].poly * steps[k + length - 1].poly;
@@ -340,9 +340,10 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
   for (const Shape& c : classes) work += (double)c.p * c.p * c.q * (double)c.members.size();
   h->parts[0] = exact || (!all_small && work <= (double)kTwoWordWork) ? 2 : 1;
   h->parts[1] = exact ? 2 : 1;
+  const bool coarse[2] = {false, cfg->x_dtype == ORTHDION_BF16};
   for (int step = 0; step < 2; ++step)
     for (int split = 0; split < 2; ++split)
-      for (int mode = 0; mode < kModes; ++mode) plan_jobs(steps, (Mode)mode, split != 0, h->parts[step], step != 0, &h->plans[step][split][mode]);
+      for (int mode = 0; mode < kModes; ++mode) plan_jobs(steps, (Mode)mode, split != 0, h->parts[step], coarse[step], &h->plans[step][split][mode]);
   // Splits; where those of the set would take more than two workgroups a CU, fewer of each (a 1024-wide model in fp32, 576 workgroups
   // 791 us a step, 432 688)
   int64_t beside = 0, groups = 0;
@@ -361,11 +362,11 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
     const int64_t elements = (int64_t)c.p * c.q;
     const int lp = pitch(c.p), lq = pitch(c.q);
     const Mode mode = mode_of(c);
-    // O in one word of few rows: 2 + 2 + 1 steps left 2.6 to 3.4e-3 on 136 x 16384 of a falling spectrum, step by step 2.2e-3 (bf16's rounding
+    // O in one word of few rows, leaving with that precision: 2 + 2 + 1 steps left 2.6 to 3.4e-3 on 136 x 16384 of a falling spectrum, step by step 2.2e-3 (bf16's rounding
     // alone 1.7e-3)
-    const Mode alone = mode == SEGMENTS && c.p < kSegmentRows && h->parts[0] == 1 ? STEP_BY_STEP : mode;
+    auto mode_of_call = [&](int step) { return mode == SEGMENTS && c.p < kSegmentRows && h->parts[step] == 1 && !coarse[step] ? STEP_BY_STEP : mode; };
     const int splits = splits_of[&c - classes.data()];
-    const Plan* const plan[2] = {&h->plans[0][splits > 0][alone], &h->plans[1][splits > 0][mode]};
+    const Plan* const plan[2] = {&h->plans[0][splits > 0][mode_of_call(0)], &h->plans[1][splits > 0][mode_of_call(1)]};
     const int symmetric = std::max(plan[0]->symmetric, plan[1]->symmetric);
     const int64_t stride = h->parts[0] * (2 * od::ns_y_plane(c.p, lq) + symmetric * od::ns_s_plane(c.p, lp)) + od::ns_partials(c.p, splits);
     for (size_t done = 0; done < c.members.size();) {

@@ -66,3 +66,16 @@ def test_adamw_of_huge_gradients(beta2, t0):
     # four roundings a moment, and of x those of the root, its factor, the sum, the quotient and the products: 16 halves of a step
     assert np.all(np.abs(v - wv) <= 6 * 2.0 ** -24 * wv) and np.all(np.abs(m - wm) <= 4 * 2.0 ** -24 * np.abs(wm))
     assert np.all(np.abs(x - wx) <= 16 * 2.0 ** -24 * np.abs(wx)), (x, wx)
+
+
+@pytest.mark.parametrize("shape", [(700, 3000), (3000, 700), (1000, 1000), (200, 16384)])
+def test_step_of_fp32_parameters_in_fast_precision_is_planned_as_the_orthogonalisation(shape):
+    """Fewer Gram matrices than O's own precision admits are for parameters of 8 bits: fp32 ones take the same O, bit by bit, as
+    the orthogonalisation gives (both in one word: p^2 q above 2^29)."""
+    import torch
+    a = torch.randn(*shape, generator=torch.Generator().manual_seed(shape[0])).to("cuda:0", torch.bfloat16)
+    opt = binding.Muon([shape], x_dtype="f32", g_dtype="bf16", precision="fast", mu=0.0, lr=-1.0, scale="none")
+    o, x, m = (torch.zeros(*shape, device="cuda:0") for _ in range(3))
+    opt.orthogonalise([a], [o])
+    opt.step([x], [a], [m])
+    assert torch.equal(x, o) and bool((o != 0).any())
