@@ -333,8 +333,11 @@ typedef struct {
   int32_t nesterov;       /* 0 or 1 */
   int32_t steps;          /* 1 .. ORTHDION_MUON_MAX_STEPS */
   float coeffs[3 * ORTHDION_MUON_MAX_STEPS];   /* a, b, c of every step.  Refused (ORTHDION_E_INVALID_ARG)
-                           * where singular values in [0, 1] could grow beyond 32, or |a + b s^2 + c s^4|
-                           * beyond 256 over the range that a step may meet */
+                           * over the range of singular values that a step may meet - [0, 1] at first, then
+                           * what the step before makes of its range, 2 % added each time for rounding - are:
+                           * values that grow beyond 32, or that a step before the last one shrinks below 2^-24
+                           * throughout; and |a + b s^2 + c s^4| above 256, or below 2^-24 throughout without
+                           * being zero */
   float mu;               /* 0 <= mu <= 1 */
   float lr, weight_decay;
   float eps;              /* >= 0 */

@@ -154,6 +154,9 @@ struct Step {
 
 // Powers of two of the stored words follow from bounds on the spectral norms, which bound every entry: sigma <= 1 at the start
 // (Frobenius norm 1), then the largest |sigma (a + b sigma^2 + c sigma^4)| over the range before, with 2 % for rounding.
+// Bounds of 2^-24 and above keep every scale and every quotient of scales within fp32 (the least, of the product S S:
+// 2^(5 - 2 (13 + 48)) = 2^-117), so steps that shrink X or P further are refused; a polynomial that is zero gives zeros under any scale.
+constexpr double kLeastBound = 1.0 / (1 << 24);
 static int plan_steps(const orthdion_muon_config& cfg, std::vector<Step>* steps) {
   double top = 1.02;
   for (int k = 0; k < cfg.steps; ++k) {
@@ -166,8 +169,10 @@ static int plan_steps(const orthdion_muon_config& cfg, std::vector<Step>* steps)
       next = std::max(next, v * x);
     }
     if (!(s.poly <= 256.0) || !(next <= 32.0)) return ORTHDION_E_INVALID_ARG;
-    s.poly = std::max(1.02 * s.poly, 1.0 / 256);
-    top = std::max(1.02 * next, 1.0 / 256);
+    // what the last step leaves is stored as fp32 or bf16
+    if ((s.poly > 0.0 && s.poly < kLeastBound) || (k + 1 < cfg.steps && next > 0.0 && next < kLeastBound)) return ORTHDION_E_INVALID_ARG;
+    s.poly = std::max(1.02 * s.poly, kLeastBound);
+    top = std::max(1.02 * next, kLeastBound);
     steps->push_back(s);
   }
   steps->push_back(Step{0.0, 0.0, 0.0, top, 1.0});            // the bound behind the last step
@@ -186,7 +191,7 @@ static double product_bound(const std::vector<Step>& steps, int from, int count)
     }
     most = std::max(most, std::fabs(z));
   }
-  return std::max(1.02 * most, 1.0 / 256);
+  return std::max(1.02 * most, kLeastBound * kLeastBound);
 }
 
 static void plan_jobs(const std::vector<Step>& steps, Mode mode, bool split, int parts, bool coarse, Plan* plan) {

@@ -61,3 +61,22 @@ def test_adamw_refuses_a_buffer_given_twice():
                 shared[other][0] = shared[written][1]
                 with pytest.raises(ValueError):
                     opt._separate_tensors(*shared)
+
+
+QUINTIC, CUBIC, CONVERGING = ((3.4445, -4.7750, 2.0315),) * 5, ((1.5, -0.5, 0.0),) * 10, ((1.875, -1.25, 0.375),) * 14
+STEEP = ((8.28721, -23.59589, 17.30039), (4.10706, -2.94785, 0.54484), (3.94869, -2.90890, 0.55182), (3.31842, -2.48849, 0.51005), (2.30065, -1.66890, 0.41881))
+
+
+@pytest.mark.parametrize("coeffs,taken", [
+    (QUINTIC, True), (CUBIC, True), (CONVERGING, True), (((1.0, 0.0, 0.0),), True), (((0.05, 0.0, 0.0),) * 4, True),
+    # the last step's result is fp32 or bf16
+    (((0.02, 0.0, 0.0),) * 5, True), (((1e-6, 0.0, 0.0),), True), (((1e-6, 0.0, 0.0),) * 2, True),
+    (((0.0, 0.0, 0.0),), True), (((0.0, 0.0, 0.0),) + QUINTIC, True),
+    (((0.01, 0.0, 0.0),) * 5, False), (((0.01, 0.0, 0.0),) * 8, False), (((1e-6, 0.0, 0.0),) * 3, False), (((1e-8, 0.0, 0.0),), False),
+    # 2 % a step for rounding: singular values just beyond 1 run away from this one
+    (STEEP, False), (tuple((x / 1.02, y / 1.02 ** 3, z / 1.02 ** 5) for x, y, z in STEEP), True)])
+def test_muon_coefficients(coeffs, taken):
+    if taken:
+        b.orthdion_muon_destroy(b.orthdion_muon_create([(64, 64)], b.ORTHDION_BF16, b.ORTHDION_BF16, coeffs=coeffs))
+    else:
+        assert status_of(lambda: b.orthdion_muon_create([(64, 64)], b.ORTHDION_BF16, b.ORTHDION_BF16, coeffs=coeffs)) == b.ORTHDION_E_INVALID_ARG

@@ -4,8 +4,9 @@ import math
 import numpy as np
 import pytest
 
-from oracle.optimizers_oracle import adamw_step
+from oracle.optimizers_oracle import adamw_step, newton_schulz
 from paper_2605_16341_amd import binding
+from test_gpu_muon import check, matrix, tolerance
 
 pytestmark = pytest.mark.gpu
 
@@ -79,3 +80,33 @@ def test_step_of_fp32_parameters_in_fast_precision_is_planned_as_the_orthogonali
     opt.orthogonalise([a], [o])
     opt.step([x], [a], [m])
     assert torch.equal(x, o) and bool((o != 0).any())
+
+
+@pytest.mark.parametrize("shape", [(40, 56), (300, 200), (136, 4096), (600, 1000)])
+@pytest.mark.parametrize("coeffs", [((0.02, 0.0, 0.0),) * 5, ((1e-6, 0.0, 0.0),) * 2, ((0.05, -0.03, 0.0), (0.001, 0.0, 0.0), (3.0, 0.0, 0.0), (5.0, 0.0, 0.0)),
+                                    ((1e-5, 0.0, 0.0), (12.0, 0.0, 0.0), (12.0, 0.0, 0.0), (12.0, 0.0, 0.0))])
+@pytest.mark.parametrize("precision", ["exact", "fast"])
+def test_coefficients_that_shrink(shape, coeffs, precision):
+    """Iterates far below 1 keep the bits of their words."""
+    import torch
+    a = matrix(np.random.default_rng(12), *shape)
+    opt = binding.Muon([shape], x_dtype="f32", precision=precision, coeffs=coeffs, mu=0.0, lr=-1.0, scale="none")
+    A = torch.from_numpy(a).to("cuda:0", torch.float32)
+    o, x, m = (torch.zeros(*shape, device="cuda:0") for _ in range(3))
+    opt.orthogonalise([A], [o])
+    opt.step([x], [A], [m])
+    host = A.double().cpu().numpy()
+    want = newton_schulz(host, coeffs)
+    for got in (o, x):
+        check(got, want, tolerance(host, coeffs, precision == "exact", "f32"))
+
+
+@pytest.mark.parametrize("coeffs", [((0.0, 0.0, 0.0),), ((0.0, 0.0, 0.0),) + binding.MUON_COEFFS, binding.MUON_COEFFS + ((0.0, 0.0, 0.0),)])
+@pytest.mark.parametrize("shape", [(40, 56), (300, 200), (600, 1000)])
+def test_a_polynomial_that_is_zero_gives_zeros(coeffs, shape):
+    import torch
+    opt = binding.Muon([shape], x_dtype="bf16", coeffs=coeffs)
+    a = torch.from_numpy(matrix(np.random.default_rng(13), *shape)).to("cuda:0", torch.bfloat16)
+    o = torch.ones_like(a)
+    opt.orthogonalise([a], [o])
+    assert bool((o == 0).all()) and opt.info() == [0]
