@@ -331,9 +331,9 @@ def orthdion_muon_create(shapes: Sequence[Sequence[int]], x_dtype: int, g_dtype:
     for i, (m, n) in enumerate(shapes):
         ld = lds[i] if lds is not None else (n, n, n)
         descs[i] = orthdion_muon_matdesc(int(m), int(n), int(ld[0]), int(ld[1]), int(ld[2]), 1.0 if scales is None else float(scales[i]))
-    flat = [float(v) for step in coeffs for v in step]
-    if len(flat) != 3 * len(coeffs) or len(coeffs) > ORTHDION_MUON_MAX_STEPS:
+    if any(len(step) != 3 for step in coeffs) or len(coeffs) > ORTHDION_MUON_MAX_STEPS:
         raise ValueError(f"coeffs: at most {ORTHDION_MUON_MAX_STEPS} triples (a, b, c)")
+    flat = [float(v) for step in coeffs for v in step]
     cfg = orthdion_muon_config(int(x_dtype), int(g_dtype), int(precision), int(nesterov), len(coeffs),
                                (ctypes.c_float * (3 * ORTHDION_MUON_MAX_STEPS))(*flat), float(mu), float(lr), float(weight_decay), float(eps))
     handle = ctypes.c_void_p()

@@ -80,3 +80,9 @@ def test_muon_coefficients(coeffs, taken):
         b.orthdion_muon_destroy(b.orthdion_muon_create([(64, 64)], b.ORTHDION_BF16, b.ORTHDION_BF16, coeffs=coeffs))
     else:
         assert status_of(lambda: b.orthdion_muon_create([(64, 64)], b.ORTHDION_BF16, b.ORTHDION_BF16, coeffs=coeffs)) == b.ORTHDION_E_INVALID_ARG
+
+
+@pytest.mark.parametrize("coeffs", [((1.0, 0.0), (0.0, 1.0, 0.0, 0.0)), ((1.0, 0.0, 0.0, 0.0), (1.0, 0.0)), ((1.0, 0.0),), ((1.0, 0.0, 0.0),) * 33])
+def test_muon_coefficients_are_triples(coeffs):
+    with pytest.raises(ValueError):
+        b.orthdion_muon_create([(64, 64)], b.ORTHDION_BF16, b.ORTHDION_BF16, coeffs=coeffs)
