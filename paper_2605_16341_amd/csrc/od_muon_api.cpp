@@ -22,6 +22,10 @@ constexpr int64_t kMaxDim = 1 << 22;       // 32-bit offsets of the operand load
 // Matrices step together (a cluster: every kernel of the iteration is one launch over it) up to this many elements; the
 // next cluster reuses the workspace (24 decoder layers: 2^28 42.0, 2^29 41.0, 2^30 40.8 ms and twice the workspace).
 constexpr int64_t kClusterElements = (int64_t)1 << 29;
+// A slice is counted as the elements that it would be at this many words each, if those are more: thin matrices take more by the
+// padding of their rows and by their partial sums (4 x 100000: 35 words an element), those of more than 128 rows up to 7.5.  So no
+// cluster takes more workspace than 8.6 GB, 17.2 in two words, unless one matrix does.
+constexpr int64_t kSliceWords = 8;
 // Elements behind one partial sum of squares, while those are fewer than kMuonParts.  With 16384 the odd matrix of six small
 // ones (201 x 327) took 24 us, the time of a thread's chain of single loads.
 constexpr int64_t kPartElements = 2048;
@@ -364,7 +368,6 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
   int64_t held = 0;
   size_t slices = 0, most = 0;
   for (const Shape& c : classes) {
-    const int64_t elements = (int64_t)c.p * c.q;
     const int lp = pitch(c.p), lq = pitch(c.q);
     const Mode mode = mode_of(c);
     // O in one word of few rows, leaving with that precision: 2 + 2 + 1 steps left 2.6 to 3.4e-3 on 136 x 16384 of a falling spectrum, step by step 2.2e-3 (bf16's rounding
@@ -374,6 +377,7 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
     const Plan* const plan[2] = {&h->plans[0][splits > 0][mode_of_call(0)], &h->plans[1][splits > 0][mode_of_call(1)]};
     const int symmetric = std::max(plan[0]->symmetric, plan[1]->symmetric);
     const int64_t stride = h->parts[0] * (2 * od::ns_y_plane(c.p, lq) + symmetric * od::ns_s_plane(c.p, lp)) + od::ns_partials(c.p, splits);
+    const int64_t elements = std::max((int64_t)c.p * c.q, stride / (kSliceWords * h->parts[0]));
     for (size_t done = 0; done < c.members.size();) {
       if (h->clusters.empty() || held + elements > kClusterElements || (int)h->clusters.back().classes.size() == od::kNsClasses) {
         h->clusters.push_back(Cluster{});

@@ -86,3 +86,17 @@ def test_muon_coefficients(coeffs, taken):
 def test_muon_coefficients_are_triples(coeffs):
     with pytest.raises(ValueError):
         b.orthdion_muon_create([(64, 64)], b.ORTHDION_BF16, b.ORTHDION_BF16, coeffs=coeffs)
+
+
+@pytest.mark.parametrize("shape,count", [((4, 100000), 1000), ((1, 4000000), 100), ((100000, 4), 1000), ((1, 512), 1 << 17), ((129, 129), 32000)])
+@pytest.mark.parametrize("dtype", [b.ORTHDION_BF16, b.ORTHDION_F32])
+def test_muon_workspace_of_many_thin_matrices_is_bounded(shape, count, dtype):
+    """At most 2^29 elements of 8 words of two bytes (two words a value in fp32) step together, or one matrix, beside the tables:
+    a matrix's pointers, shape and 256 sums."""
+    def need(n):
+        h = b.orthdion_muon_create([shape] * n, dtype, dtype)
+        got = b.orthdion_muon_workspace_bytes(h)
+        b.orthdion_muon_destroy(h)
+        return got
+    words = 1 if dtype == b.ORTHDION_BF16 else 2
+    assert need(count) <= max(2 ** 29 * 8 * 2 * words, need(1)) + count * 2300 + 2048

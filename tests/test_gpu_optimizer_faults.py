@@ -110,3 +110,28 @@ def test_a_polynomial_that_is_zero_gives_zeros(coeffs, shape):
     o = torch.ones_like(a)
     opt.orthogonalise([a], [o])
     assert bool((o == 0).all()) and opt.info() == [0]
+
+
+def test_thin_matrices_beyond_what_steps_together():
+    """Rows so long that their padding fills a cluster's workspace with 84 of them: the later ones take it over from the earlier."""
+    import torch
+    n, count = 400000, 170
+    gen = torch.Generator(device="cuda:0").manual_seed(11)
+    a = torch.randn(count, 1, n, device="cuda:0", generator=gen).bfloat16()
+    o = torch.empty_like(a)
+    opt = binding.Muon([(1, n)] * count, x_dtype="bf16")
+    assert opt.workspace_bytes < 9 * 10 ** 9
+    opt.orthogonalise(list(a), list(o))
+    alone = binding.Muon([(1, n)], x_dtype="bf16")
+    for k in (0, 1, 82, 83, 84, 85, 167, 168, 169):
+        single = torch.empty_like(a[k])
+        alone.orthogonalise([a[k]], [single])
+        assert torch.equal(o[k], single), k
+    assert opt.info() == [0] * count
+    # a single row keeps its direction: O is the iteration of 1 times the row over its norm
+    s = 1.0
+    for ca, cb, cc in binding.MUON_COEFFS:
+        s = ca * s + cb * s ** 3 + cc * s ** 5
+    want = s * a.double() / a.double().norm(dim=2, keepdim=True)
+    # one word of Y and P: 2^-11 twice a step of five; later steps' slopes at s = 0.70, 1.11, 0.72, 1.09 multiply that by 1.42 at most; bf16
+    assert float(((o.double() - want).norm(dim=2) / want.norm(dim=2)).max()) <= 10 * 2.0 ** -11 * 2 + 2.0 ** -8
