@@ -347,6 +347,12 @@ int orthdion_muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc*
                          const orthdion_muon_config* cfg);
 /* Bytes of device scratch of a call, 256-byte aligned; 0 for a NULL handle. */
 size_t orthdion_muon_workspace_bytes(orthdion_muon_handle h);
+/* The tiles that the products of an orthogonalisation (step = 0) or a step (1) are computed on, for tuning and tests:
+ * the sum of 1, 2, 4 and 8 for tiles of 64, 128, 192 and 256 in use, 0 where there is no such product.
+ * tiles[0] Gram matrices, [1] symmetric p x p products, [2] products with the matrix, [3] p x p products that are
+ * not mirrored, the last product of [4] wide and square matrices, [5] tall ones. */
+#define ORTHDION_MUON_PRODUCTS 6
+int orthdion_muon_get_tiles(orthdion_muon_handle h, int32_t step, int32_t tiles[ORTHDION_MUON_PRODUCTS]);
 int orthdion_muon_set_lr(orthdion_muon_handle h, float lr);
 int orthdion_muon_set_mu(orthdion_muon_handle h, float mu);
 int orthdion_muon_set_weight_decay(orthdion_muon_handle h, float weight_decay);

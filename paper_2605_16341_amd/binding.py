@@ -33,7 +33,7 @@ EXPORTS = ["orthdion_create", "orthdion_workspace_bytes", "orthdion_set_lr", "or
            "orthdion_profile_begin", "orthdion_profile_end", "orthdion_set_diagnostics",
            "orthdion_get_diagnostics", "orthdion_rank_policy", "orthdion_resize_q", "orthdion_strerror",
            "orthdion_destroy", "orthdion_step_static", "orthdion_static_scratch_bytes", "orthdion_get_warnings",
-           "orthdion_get_groups", "orthdion_muon_create", "orthdion_muon_workspace_bytes", "orthdion_muon_set_lr",
+           "orthdion_get_groups", "orthdion_muon_create", "orthdion_muon_workspace_bytes", "orthdion_muon_get_tiles", "orthdion_muon_set_lr",
            "orthdion_muon_set_mu", "orthdion_muon_set_weight_decay", "orthdion_muon_step", "orthdion_muon_orthogonalise",
            "orthdion_muon_get_info", "orthdion_muon_destroy", "orthdion_adamw_create", "orthdion_adamw_set_lr",
            "orthdion_adamw_step", "orthdion_adamw_destroy"]
@@ -162,7 +162,8 @@ def load() -> ctypes.CDLL:
     pp, f32 = ctypes.POINTER(vp), ctypes.c_float
     for name, args, res in (
             ("orthdion_muon_create", [pp, ctypes.POINTER(orthdion_muon_matdesc), ctypes.c_int32, ctypes.POINTER(orthdion_muon_config)], ctypes.c_int),
-            ("orthdion_muon_workspace_bytes", [vp], sz), ("orthdion_muon_set_lr", [vp, f32], ctypes.c_int),
+            ("orthdion_muon_workspace_bytes", [vp], sz),
+            ("orthdion_muon_get_tiles", [vp, ctypes.c_int32, ctypes.POINTER(ctypes.c_int32)], ctypes.c_int), ("orthdion_muon_set_lr", [vp, f32], ctypes.c_int),
             ("orthdion_muon_set_mu", [vp, f32], ctypes.c_int), ("orthdion_muon_set_weight_decay", [vp, f32], ctypes.c_int),
             ("orthdion_muon_step", [vp, pp, pp, pp, vp, sz, vp], ctypes.c_int),
             ("orthdion_muon_orthogonalise", [vp, pp, pp, vp, sz, vp], ctypes.c_int),
@@ -343,6 +344,17 @@ def orthdion_muon_create(shapes: Sequence[Sequence[int]], x_dtype: int, g_dtype:
 
 def orthdion_muon_workspace_bytes(handle: int) -> int:
     return int(load().orthdion_muon_workspace_bytes(handle))
+
+
+# kinds of products as orthdion_muon_get_tiles counts them
+MUON_PRODUCTS = ("gram", "symmetric", "apply", "full", "last_wide", "last_tall")
+
+
+def orthdion_muon_get_tiles(handle: int, step: bool) -> dict:
+    """Widths of the tiles that each kind of product is computed on, as a set; kinds that a call has none of are left out."""
+    out = (ctypes.c_int32 * len(MUON_PRODUCTS))()
+    _check(load().orthdion_muon_get_tiles(handle, int(step), out))
+    return {name: {64 * (k + 1) for k in range(4) if bits >> k & 1} for name, bits in zip(MUON_PRODUCTS, out) if bits}
 
 
 def orthdion_muon_set_lr(handle: int, lr: float) -> None:

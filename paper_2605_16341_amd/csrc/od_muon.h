@@ -97,6 +97,9 @@ struct MuonTables {                        // in the workspace, one row per matr
   int* info;                               // 1: a non-finite entry
 };
 
+// width of the tiles that the products of a launch are computed on
+int ns_tile(const NsArgs& a, int parts);
+
 // M = mu M + G and the partial sums of squares of B; copies the pointers and shapes of `count` matrices
 // (rows mat0 ..) into the tables.  entries[i].M null: B = G.
 hipError_t launch_muon_begin(const MuonEntry* entries, const MuonMat* mats, int mat0, int count, const MuonTables& t, float mu,

@@ -949,19 +949,20 @@ int tiles_of(const NsJob& c) {
   return c.kind == NS_APPLY ? n * ceil_div(c.q, T) : c.kind == NS_FULL ? n * n : n * (n + 1) / 2 * (c.splits > 0 ? c.splits : 1);
 }
 
-// f with the tile for these jobs: the one with the least time in us by what a step of 64 k and a workgroup's beginning and
+}  // namespace
+
+// The tile for these jobs: the one with the least time in us by what a step of 64 k and a workgroup's beginning and
 // end take.  256 CUs; beyond one round of workgroups the last one counts half by what is in it, half as a whole one.
 // One word: 64 x 64 0.43 a step, 0.30 for each workgroup of a CU where there are more, and 4; 128 x 128 0.7 and 4 alone on a CU, 1.0
 // and 5 for two side by side, 1.2 where that happens everywhere and the clock gives way; 192 x 192 1.15 and 6, 1.43 in several
 // rounds; 256 x 256 1.7 and 8, 1.85 with most CUs at work.
 // Two words: 64 x 64 0.8 and 0.65, 128 x 128 1.7 a round (one workgroup fits a CU), 256 x 256 5.2 and 6.3 (three passes).
 // Measured on products of 264 x 264 to 4096 x 4096, 1 to 72 matrices: the rule takes the fastest or one within 10 %.
-template <class F>
-hipError_t with_tile(const NsArgs& a, int parts, F&& f) {
+int ns_tile(const NsArgs& a, int parts) {
   double n64 = 0.0, n128 = 0.0, n192 = 0.0, n256 = 0.0, steps = 0.0;
   for (int k = 0; k < a.count; ++k) {
     const NsJob& j = a.j[k];
-    if (j.splits > 0) return f(Small{});               // partial sums
+    if (j.splits > 0) return Small::T;                 // partial sums
     const double nb = j.nb, n = nb * tiles_of<256>(j);
     n64 += nb * tiles_of<64>(j);
     n128 += nb * tiles_of<128>(j);
@@ -985,7 +986,20 @@ hipError_t with_tile(const NsArgs& a, int parts, F&& f) {
   }
   t192 *= 1.07;                                        // the least even of the four: taken where it is clearly ahead
   const double least = std::min(std::min(t64, t128), std::min(t192, t256));
-  return least == t64 ? f(Tiny{}) : least == t128 ? f(Small{}) : least == t192 ? f(Mid{}) : f(Large{});
+  return least == t64 ? Tiny::T : least == t128 ? Small::T : least == t192 ? Mid::T : Large::T;
+}
+
+namespace {
+
+// f with that tile
+template <class F>
+hipError_t with_tile(const NsArgs& a, int parts, F&& f) {
+  switch (ns_tile(a, parts)) {
+    case Tiny::T: return f(Tiny{});
+    case Small::T: return f(Small{});
+    case Mid::T: return f(Mid{});
+    default: return f(Large{});
+  }
 }
 
 template <class TL, int PARTS, bool XBF>

@@ -425,6 +425,56 @@ static int muon_create(orthdion_muon_handle* out, const orthdion_muon_matdesc* m
     if ((expr) != hipSuccess) return ORTHDION_E_HIP;   \
   } while (0)
 
+// The launches of one cluster behind the input's norm, in order: f(what, jobs, steps of a NS_SMALL launch).
+enum Launch { SCALE, PRODUCTS, REDUCE, SMALL_STEPS, LAST };
+template <class F>
+static int for_launches(orthdion_muon_handle h, const Cluster& cl, bool update, char* slices, F&& f) {
+  const int parts = h->parts[update];
+  NsArgs args;
+  auto add = [&](const Class& c, const PlannedJob& job) {
+    NsJob& j = args.j[args.count++];
+    j = c.job;
+    j.base = reinterpret_cast<uint16_t*>(slices + c.offset);
+    auto at = [&](const Operand& o) {
+      const int64_t y = od::ns_y_plane(j.p, j.lq) * parts, s = od::ns_s_plane(j.p, j.lp) * parts;
+      return o.where == IN_Y ? o.index * y : 2 * y + (o.where == IN_SYMMETRIC ? o.index : c.symmetric) * s;
+    };
+    j.kind = job.kind;
+    j.a = at(job.a); j.b = at(job.b); j.e = at(job.e); j.out = at(job.out);
+    j.ca = job.ca; j.cb = job.cb; j.cc = job.cc;
+    j.splits = job.kind == od::NS_GRAM || job.kind == od::NS_REDUCE || job.kind == od::NS_SMALL ? c.splits : 0;
+  };
+  args.count = 0;
+  size_t stages = 0;
+  for (const Class& c : cl.classes) {
+    add(c, c.plan[update]->last);
+    stages = std::max(stages, c.plan[update]->stages.size());
+  }
+  OD_TRY(f(SCALE, args, nullptr));
+  const NsArgs last = args;
+  // the jobs of stage s that `of` takes; the plan of the last of them
+  auto gather = [&](size_t s, auto&& of) {
+    const Plan* plan = nullptr;
+    args.count = 0;
+    for (const Class& c : cl.classes)
+      if (s < c.plan[update]->stages.size())
+        for (const PlannedJob& job : c.plan[update]->stages[s])
+          if (of(job.kind)) {
+            add(c, job);
+            plan = c.plan[update];
+          }
+    return plan;
+  };
+  for (size_t s = 0; s < stages; ++s) {
+    if (gather(s, [](od::NsKind k) { return k <= od::NS_FULL; })) OD_TRY(f(PRODUCTS, args, nullptr));
+    if (gather(s, [](od::NsKind k) { return k == od::NS_REDUCE; })) OD_TRY(f(REDUCE, args, nullptr));
+    // small matrices take three stages a segment
+    if (const Plan* plan = gather(s, [](od::NsKind k) { return k == od::NS_SMALL; })) OD_TRY(f(SMALL_STEPS, args, &plan->steps[s / 3]));
+  }
+  OD_TRY(f(LAST, last, nullptr));
+  return ORTHDION_OK;
+}
+
 // X and M null: orthdion_muon_orthogonalise (A at G, O at X)
 static int muon_run(orthdion_muon_handle h, void* const* X, const void* const* G, float* const* M, bool update, void* workspace,
                     size_t workspace_bytes, void* stream) {
@@ -455,49 +505,17 @@ static int muon_run(orthdion_muon_handle h, void* const* X, const void* const* G
   const float keep = (float)(1.0 - (double)h->cfg.lr * (double)h->cfg.weight_decay);
   const int parts = h->parts[update];
   for (const Cluster& cl : h->clusters) {
-    NsArgs args;
-    auto add = [&](const Class& c, const PlannedJob& job) {
-      NsJob& j = args.j[args.count++];
-      j = c.job;
-      j.base = reinterpret_cast<uint16_t*>(ws + h->off_slices + c.offset);
-      auto at = [&](const Operand& o) {
-        const int64_t y = od::ns_y_plane(j.p, j.lq) * parts, s = od::ns_s_plane(j.p, j.lp) * parts;
-        return o.where == IN_Y ? o.index * y : 2 * y + (o.where == IN_SYMMETRIC ? o.index : c.symmetric) * s;
-      };
-      j.kind = job.kind;
-      j.a = at(job.a); j.b = at(job.b); j.e = at(job.e); j.out = at(job.out);
-      j.ca = job.ca; j.cb = job.cb; j.cc = job.cc;
-      j.splits = job.kind == od::NS_GRAM || job.kind == od::NS_REDUCE || job.kind == od::NS_SMALL ? c.splits : 0;
-    };
     OD_TRY(od::launch_muon_begin(entries.get() + cl.mat0, h->table.data() + cl.mat0, cl.mat0, cl.count, t, h->cfg.mu, nesterov, gbf, st));
-    args.count = 0;
-    size_t stages = 0;
-    for (const Class& c : cl.classes) {
-      add(c, c.plan[update]->last);
-      stages = std::max(stages, c.plan[update]->stages.size());
-    }
-    OD_TRY(od::launch_muon_scale(args, t, h->cfg.mu, nesterov, gbf, parts, h->cfg.eps, std::ldexp(1.0, h->first_exp), st));
-    const NsArgs last = args;
-    // the jobs of stage s that `of` takes; the plan of the last of them
-    auto gather = [&](size_t s, auto&& of) {
-      const Plan* plan = nullptr;
-      args.count = 0;
-      for (const Class& c : cl.classes)
-        if (s < c.plan[update]->stages.size())
-          for (const PlannedJob& job : c.plan[update]->stages[s])
-            if (of(job.kind)) {
-              add(c, job);
-              plan = c.plan[update];
-            }
-      return plan;
-    };
-    for (size_t s = 0; s < stages; ++s) {
-      if (gather(s, [](od::NsKind k) { return k <= od::NS_FULL; })) OD_TRY(od::launch_ns_products(args, parts, st));
-      if (gather(s, [](od::NsKind k) { return k == od::NS_REDUCE; })) OD_TRY(od::launch_ns_reduce(args, parts, st));
-      // small matrices take three stages a segment
-      if (const Plan* plan = gather(s, [](od::NsKind k) { return k == od::NS_SMALL; })) OD_TRY(od::launch_ns_small(args, plan->steps[s / 3], parts, st));
-    }
-    OD_TRY(od::launch_ns_final(last, t, parts, update, keep, h->cfg.lr, xbf, st));
+    const int rc = for_launches(h, cl, update, ws + h->off_slices, [&](Launch what, const NsArgs& args, const od::NsSteps* steps) {
+      switch (what) {
+        case SCALE: return od::launch_muon_scale(args, t, h->cfg.mu, nesterov, gbf, parts, h->cfg.eps, std::ldexp(1.0, h->first_exp), st);
+        case PRODUCTS: return od::launch_ns_products(args, parts, st);
+        case REDUCE: return od::launch_ns_reduce(args, parts, st);
+        case SMALL_STEPS: return od::launch_ns_small(args, *steps, parts, st);
+        default: return od::launch_ns_final(args, t, parts, update, keep, h->cfg.lr, xbf, st);
+      }
+    });
+    if (rc != ORTHDION_OK) return rc;
   }
   return ORTHDION_OK;
 }
@@ -517,6 +535,23 @@ extern "C" int orthdion_muon_create(orthdion_muon_handle* out, const orthdion_mu
 }
 
 extern "C" size_t orthdion_muon_workspace_bytes(orthdion_muon_handle h) { return h ? h->ws_bytes : 0; }
+
+extern "C" int orthdion_muon_get_tiles(orthdion_muon_handle h, int32_t step, int32_t* tiles) {
+  if (!h || !tiles) return ORTHDION_E_NULL_PTR;
+  if (step != 0 && step != 1) return ORTHDION_E_INVALID_ARG;
+  for (int k = 0; k < ORTHDION_MUON_PRODUCTS; ++k) tiles[k] = 0;
+  for (const Cluster& cl : h->clusters) {
+    const int rc = for_launches(h, cl, step != 0, nullptr, [&](Launch what, const NsArgs& args, const od::NsSteps*) {
+      if (what == PRODUCTS || what == LAST) {
+        const int bit = 1 << (od::ns_tile(args, h->parts[step]) / 64 - 1);
+        for (int k = 0; k < args.count; ++k) tiles[what == PRODUCTS ? args.j[k].kind : args.j[k].tall ? 5 : 4] |= bit;
+      }
+      return hipSuccess;
+    });
+    if (rc != ORTHDION_OK) return rc;
+  }
+  return ORTHDION_OK;
+}
 
 extern "C" int orthdion_muon_set_lr(orthdion_muon_handle h, float lr) {
   if (!h) return ORTHDION_E_NULL_PTR;
