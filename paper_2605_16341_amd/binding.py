@@ -639,6 +639,8 @@ class Muon:
             orthdion_muon_orthogonalise(self.handle, a, o, self.workspace.data_ptr(), self.workspace_bytes, self._stream(stream))
 
     def info(self, stream=None) -> List[int]:
+        """Per matrix of the last call 0, or 1 where B (A) held a NaN or an infinity; from the workspace, so before anything else uses
+        that, where it is shared.  Waits for the stream."""
         with _on_device(self._torch, self.workspace.get_device()):
             return orthdion_muon_get_info(self.handle, self.nmat, self._stream(stream))
 

@@ -6,7 +6,8 @@ import pytest
 
 from oracle.optimizers_oracle import adamw_step, newton_schulz
 from paper_2605_16341_amd import binding
-from test_gpu_muon import check, matrix, tolerance
+from test_gpu_muon import HALF, QUINTIC, check, matrix, tolerance
+from test_gpu_muon_tiles import tolerance as tolerances
 
 pytestmark = pytest.mark.gpu
 
@@ -135,3 +136,30 @@ def test_thin_matrices_beyond_what_steps_together():
     want = s * a.double() / a.double().norm(dim=2, keepdim=True)
     # one word of Y and P: 2^-11 twice a step of five; later steps' slopes at s = 0.70, 1.11, 0.72, 1.09 multiply that by 1.42 at most; bf16
     assert float(((o.double() - want).norm(dim=2) / want.norm(dim=2)).max()) <= 10 * 2.0 ** -11 * 2 + 2.0 ** -8
+
+
+@pytest.mark.parametrize("power", [1, 2])
+@pytest.mark.parametrize("shape", [(96, 160), (300, 200), (136, 4096), (136, 16384), (520, 1300), (3000, 700), (1000, 1000)])
+@pytest.mark.parametrize("g", ["bf16", "f32"])
+def test_falling_spectra(power, shape, g):
+    """Singular values 1 / i and 1 / i^2: rounding to u of the largest is u i^2 of the i-th, and the iteration brings all of them
+    towards 1: one word leaves 2 % of O on 1 / i^2.  The tolerance is that from the spectrum, by the squares of the expected errors."""
+    import torch
+    rng = np.random.default_rng(31)
+    p = min(shape)
+    u, v = (np.linalg.qr(rng.standard_normal((d, p)))[0] for d in shape)
+    dt = torch.bfloat16 if g == "bf16" else torch.float32
+    A = torch.from_numpy((u * np.arange(1.0, p + 1) ** -power) @ v.T).to("cuda:0", dt)
+    host = A.double().cpu().numpy()
+    want = newton_schulz(host, QUINTIC)
+    s = np.linalg.svd(host / (np.linalg.norm(host) + 1e-7), compute_uv=False)
+    spread = tolerances(s, max(shape), g == "f32")[1]
+    opt = binding.Muon([shape], x_dtype="f32", g_dtype=g, precision="fast" if g == "bf16" else "exact")
+    o = torch.zeros(shape, device="cuda:0")
+    opt.orthogonalise([A], [o])
+    step = binding.Muon([shape], x_dtype=g, mu=0.0, lr=-1.0, scale="none")
+    x, m = torch.zeros_like(A), torch.zeros(shape, device="cuda:0")
+    step.step([x], [A], [m])
+    for got, room in ((o, 3 * spread + HALF["f32"]), (x, 2 * 3 * spread + HALF[g])):
+        off = np.linalg.norm(got.double().cpu().numpy() - want) / np.linalg.norm(want)
+        assert off <= room, (off, room)
