@@ -1,7 +1,8 @@
 // AdamW with decoupled weight decay over a list of tensors of any lengths: one elementwise pass,
 //   m = b1 m + (1 - b1) g,   v = b2 v + (1 - b2) g^2,   t = t + 1,
 //   x = (1 - lr wd) x - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
-// HBM bound: g read, x, m and v read and written, 22 bytes an element in bf16 and 28 in fp32.  The tensors' pointers
+// HBM bound: g read, x, m and v read and written, 22 bytes an element in bf16 and 28 in fp32 (131 million bf16 elements 546 us,
+// 5.29 TB/s; a copy of 4 GiB reaches 4.73).  The tensors' pointers
 // travel in the launch's arguments, so a list of up to kAdamChunk tensors is one launch and needs no workspace.  t lives
 // in device memory, where a captured graph finds it advanced at every replay: all workgroups read it, the last
 // one of the last launch to finish adds one.
@@ -21,7 +22,7 @@ constexpr int64_t kMostLength = (int64_t)1 << 35;
 
 namespace od {
 
-constexpr int kAdamChunk = 56;             // tensors of a launch: their records fill the 4 KB of its arguments
+constexpr int kAdamChunk = 56;             // tensors of a launch: 56 bytes each, 3.2 of the 4 KB of its arguments
 constexpr int kAdamThreads = 256;
 constexpr int kAdamSpan = 4096;            // elements of a workgroup
 
@@ -43,6 +44,8 @@ struct AdamArgs {
   double beta1, beta2;
   float eps;
 };
+
+static_assert(sizeof(AdamTensor) == 56 && sizeof(AdamArgs) <= 4096, "arguments of a launch");
 
 OD_DEV double power(double x, int n) {
   double r = 1.0;
