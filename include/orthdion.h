@@ -312,10 +312,11 @@ int orthdion_step_static(orthdion_handle h, void* const* X, const void* const* G
  * coefficients and call, and in FAST a step of bf16 X joins more of them than one of fp32 X.  So the rounding of
  * one matrix's O depends on the set that it is in.  Repeated calls on the same buffers give the same bits.
  * Relative error of O (Frobenius norm) with the published coefficients, measured on matrices of up to 1000 rows:
- * FAST 0.5 to 4e-3 where the singular values fall no faster than 1 / i, 2e-2 where they fall like 1 / i^2; EXACT
- * 1 to 5e-6 and 1 to 3e-5.  Words are rounded relative to the largest singular values, and the iteration raises
- * the small ones with their errors: coefficients that raise them further (14 steps of (1.875, -1.25, 0.375)) leave
- * up to 0.12 in FAST on 1 / i^2, 9e-5 in EXACT.
+ * FAST 0.5 to 4e-3 where the singular values fall no faster than 1 / i, 2e-2 where they fall like 1 / i^2, 2 to
+ * 4e-2 on matrices of rank 8 to 32, 0.1 of rank 1; EXACT 1 to 5e-6, 1 to 3e-5, 1 to 6e-5 and 2e-4.  Words are rounded
+ * relative to the largest singular values, and the iteration raises what is small, the rounding of zeros included,
+ * by up to 3.4445^5: coefficients that raise it further leave more (14 steps of (1.875, -1.25, 0.375) on 1 / i^2 up
+ * to 0.12 in FAST, 9e-5 in EXACT).
  * A zero matrix gives X_steps = 0.  A matrix with a NaN or an infinity in B gives NaN everywhere in
  * X (or O) and 1 in orthdion_muon_get_info; other matrices of the set are not affected.
  *

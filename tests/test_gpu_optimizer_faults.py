@@ -138,18 +138,21 @@ def test_thin_matrices_beyond_what_steps_together():
     assert float(((o.double() - want).norm(dim=2) / want.norm(dim=2)).max()) <= 10 * 2.0 ** -11 * 2 + 2.0 ** -8
 
 
-@pytest.mark.parametrize("power", [1, 2])
+@pytest.mark.parametrize("spectrum", ["1/i", "1/i^2", "rank 1", "rank 8"])
 @pytest.mark.parametrize("shape", [(96, 160), (300, 200), (136, 4096), (136, 16384), (520, 1300), (3000, 700), (1000, 1000)])
 @pytest.mark.parametrize("g", ["bf16", "f32"])
-def test_falling_spectra(power, shape, g):
-    """Singular values 1 / i and 1 / i^2: rounding to u of the largest is u i^2 of the i-th, and the iteration brings all of them
-    towards 1: one word leaves 2 % of O on 1 / i^2.  The tolerance is that from the spectrum, by the squares of the expected errors."""
+def test_falling_spectra(spectrum, shape, g):
+    """Rounding to u of the largest singular value is u i^2 of the i-th of 1 / i^2, and makes small ones of zeros; the iteration brings all
+    of them towards 1: one word leaves 2 % of O on 1 / i^2, 10 % of a matrix of rank 1.  The tolerance is that from the spectrum, by
+    the squares of the expected errors."""
     import torch
     rng = np.random.default_rng(31)
     p = min(shape)
     u, v = (np.linalg.qr(rng.standard_normal((d, p)))[0] for d in shape)
+    i = np.arange(1.0, p + 1)
+    values = {"1/i": 1 / i, "1/i^2": 1 / i ** 2, "rank 1": i <= 1, "rank 8": i <= 8}[spectrum]
     dt = torch.bfloat16 if g == "bf16" else torch.float32
-    A = torch.from_numpy((u * np.arange(1.0, p + 1) ** -power) @ v.T).to("cuda:0", dt)
+    A = torch.from_numpy((u * values) @ v.T).to("cuda:0", dt)
     host = A.double().cpu().numpy()
     want = newton_schulz(host, QUINTIC)
     s = np.linalg.svd(host / (np.linalg.norm(host) + 1e-7), compute_uv=False)
