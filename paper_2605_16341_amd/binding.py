@@ -561,6 +561,9 @@ class Muon:
     scale    factor of every matrix's update: "none" (1), "spectral" (sqrt(max(1, m / n))), "rms" (0.2 sqrt(max(m, n)), the
              root mean square of an AdamW update), or a list of numbers
     lds      (ldx, ldg, ldm) per matrix where rows are further apart than n elements, e.g. parts of a fused projection
+
+    A captured step is replayed with the lr, mu and weight decay of its capture, and on this object's workspace: the object has to
+    live as long as the graph.
     """
 
     def __init__(self, shapes, x_dtype="bf16", g_dtype=None, precision="auto", mu=0.95, lr=0.02, weight_decay=0.0, nesterov=True,
@@ -667,7 +670,7 @@ class Muon:
 
 class AdamW:
     """Owns a handle of the AdamW step over a list of tensors; `lengths` are their numbers of elements.  `weight_decay` and
-    `lr_scale` are one number or one per tensor."""
+    `lr_scale` are one number or one per tensor.  A captured step is replayed with the lr of its capture."""
 
     def __init__(self, lengths, x_dtype="bf16", g_dtype=None, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, lr_scale=1.0):
         import torch
