@@ -85,7 +85,8 @@ def test_step_of_fp32_parameters_in_fast_precision_is_planned_as_the_orthogonali
 
 @pytest.mark.parametrize("shape", [(40, 56), (300, 200), (136, 4096), (600, 1000)])
 @pytest.mark.parametrize("coeffs", [((0.02, 0.0, 0.0),) * 5, ((1e-6, 0.0, 0.0),) * 2, ((0.05, -0.03, 0.0), (0.001, 0.0, 0.0), (3.0, 0.0, 0.0), (5.0, 0.0, 0.0)),
-                                    ((1e-5, 0.0, 0.0), (12.0, 0.0, 0.0), (12.0, 0.0, 0.0), (12.0, 0.0, 0.0))])
+                                    ((1e-5, 0.0, 0.0), (12.0, 0.0, 0.0), (12.0, 0.0, 0.0), (12.0, 0.0, 0.0)),
+                                    ((7e-8, 0.0, 0.0), (200.0, -100.0, 50.0), (250.0, 0.0, 0.0)), ((30.0, 0.0, 0.0), (7e-8, 0.0, 0.0), (200.0, 0.0, 0.0))])
 @pytest.mark.parametrize("precision", ["exact", "fast"])
 def test_coefficients_that_shrink(shape, coeffs, precision):
     """Iterates far below 1 keep the bits of their words."""
